@@ -253,6 +253,122 @@ llsa_status llsa_stage_timing_end(double *ms_sum, int32_t *brackets);
 llsa_status llsa_calibrate_mfma(float *out, int32_t iters, int32_t workgroups, void *hip_stream);
 llsa_status llsa_calibrate_copy(const void *src, void *dst, int64_t bytes, void *hip_stream);
 
+/*
+ * ---- dense attention: every key that a query may see, without selection ----
+ * For the layers of a model that stay dense beside the sparse ones (low resolutions, conditioning tokens, one new token over the
+ * keys so far) and as what a sparse layer is held against.
+ *   s[i][j] = sm_scale * q_i . k_j        for the keys that query i sees: j < nk, and with `causal` also j <= i + nk - nq
+ *   LSE[i]  = ln sum_j exp(s[i][j])       P[i][j] = exp(s[i][j] - LSE[i])        O[i] = sum_j P[i][j] v_j
+ * nq and nk: the lengths of the sequence, Nq and Nkv unless given per batch entry (q_lens, kv_lens).  Query head h reads key head
+ * h / (heads / kv_heads).  A query that sees nothing, and every row i >= nq, has O = 0, LSE = -infinity and a zero gradient; a key
+ * that no query sees, and every row j >= nk, has a zero gradient.  Such rows are written all the same, and whatever a row behind a
+ * length or a key that a query does not see holds, infinities and NaN included, reaches no result.
+ */
+typedef struct {
+    int32_t batch, heads;
+    int32_t kv_heads;   /* key / value heads; divides heads                                 */
+    int32_t d;          /* head dimension: 16, 32, 64 or 128                                */
+    int64_t Nq, Nkv;    /* rows of Q, O, LSE and of K, V per head (>= 1)                    */
+    float sm_scale;     /* <= 0 selects 1/sqrt(d)                                           */
+    int32_t dtype;      /* llsa_dtype of Q, K, V, O and the gradients                       */
+    int32_t causal;     /* 1: the last query sees every key, each one before it one fewer   */
+    int32_t kernel_path;/* 0: the tiled kernels; 1: one wave a row, in fp32 arithmetic (used as a cross-check) */
+    /* Elements between two batch entries, two heads and two tokens; channels are contiguous.  All three 0: contiguous
+       [batch, heads, N, d].  dQ has Q's strides, dK K's, dV V's, dO O's.  A stride of a dimension of more than one entry is a
+       multiple of 16 bytes; rows that are written must not overlap, rows that are only read may (a stride of 0 broadcasts). */
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+} llsa_dense_desc;
+
+typedef struct llsa_dense_plan_s llsa_dense_plan_t;
+
+/* Validate a problem and lay out its workspace (host only).  A plan holds no device state and may be shared by host threads and streams. */
+llsa_status llsa_dense_plan(const llsa_dense_desc *desc, llsa_dense_plan_t **out);
+void llsa_dense_plan_destroy(llsa_dense_plan_t *plan);
+
+/* Bytes of device workspace llsa_dense_forward (0) / llsa_dense_backward (1) need; may be 0, and the pointer then NULL.  Nothing in it
+   outlives the call, so one workspace serves calls that follow each other on a stream; calls that may overlap need one each. */
+size_t llsa_dense_workspace_bytes(const llsa_dense_plan_t *plan, int for_backward);
+
+/*
+ * Forward pass.  Q in: [batch, heads, Nq, d];  K, V in: [batch, kv_heads, Nkv, d];  O out: [batch, heads, Nq, d], all with the
+ * plan's strides;  q_lens, kv_lens in: [batch] int32 on the device, or NULL (values are clamped to 0 .. N);  LSE out: [batch, heads, Nq]
+ * fp32, contiguous.  No output may overlap an input or the other output.
+ */
+llsa_status llsa_dense_forward(const llsa_dense_plan_t *plan, const void *Q, const void *K, const void *V, const int32_t *q_lens,
+                               const int32_t *kv_lens, void *O, float *LSE, void *workspace, void *hip_stream);
+
+/*
+ * Backward pass: recomputes P from LSE.  Inputs as given to / produced by llsa_dense_forward, dO with O's strides; dQ, dK, dV out.
+ * The gradient of a shared key head is the sum over its query heads.  No output may overlap an input or another output.  The
+ * results are the same bits from call to call.  Errors beside the forward's: LLSA_ERR_BAD_SHAPE if rows of a gradient would overlap.
+ */
+llsa_status llsa_dense_backward(const llsa_dense_plan_t *plan, const void *Q, const void *K, const void *V, const int32_t *q_lens,
+                                const int32_t *kv_lens, const void *O, const float *LSE, const void *dO, void *dQ, void *dK,
+                                void *dV, void *workspace, void *hip_stream);
+
+/*
+ * ---- the norms between two blocks, fused with gate and residual ----
+ * What lies between the end of one block (`branch`: its output) and the start of the next one (`y`: its input), per token t of batch entry b:
+ *   z  = n(branch) * gain_branch      (gain_branch NULL: z = branch, no norm behind the block)
+ *   x' = x + residual_scale * gate[b] * z                                  (branch NULL: x' = x)
+ *   y  = n(x') * gain * (1 + scale[b]) + shift[b]                          (gain, scale, shift: NULL for 1, 0, 0)
+ * n(v) = (v - m) / sqrt(mean_c((v - m)^2) + eps) over the C channels, m = mean_c(v) (LLSA_NORM_LAYER) or 0 (LLSA_NORM_RMS, the
+ * QK-Norm's form).  fp32 arithmetic, one rounding of x' and of y; y is formed from the rounded x'.
+ */
+typedef enum { LLSA_NORM_RMS = 0, LLSA_NORM_LAYER = 1 } llsa_norm_kind;
+
+typedef struct {
+    int32_t batch;
+    int32_t C;              /* channels, 1 .. 8192; any number                              */
+    int64_t N;              /* tokens per batch entry                                       */
+    int32_t kind;           /* llsa_norm_kind, of both norms                                */
+    float eps;              /* >= 0                                                         */
+    float residual_scale;
+    int32_t dtype;          /* llsa_dtype of x, branch, y and their gradients [batch, N, C], contiguous */
+    int32_t mod_dtype;      /* llsa_dtype of gate, scale, shift                             */
+    int64_t mod_stride;     /* elements between their rows for two batch entries (>= C), as in a projection that makes all of them;
+                               0: one row for all batch entries, its gradient summed over them */
+} llsa_norm_desc;
+
+typedef struct llsa_norm_plan_s llsa_norm_plan_t;
+llsa_status llsa_norm_plan(const llsa_norm_desc *desc, llsa_norm_plan_t **out);
+void llsa_norm_plan_destroy(llsa_norm_plan_t *plan);
+size_t llsa_norm_workspace_bytes(const llsa_norm_plan_t *plan);   /* of llsa_norm_backward; the forward needs none */
+
+/* x, branch in; gain_branch, gain: [C] fp32; x_out: x' (required with a branch, not written without one; may be x's or branch's buffer);
+   y: may be NULL (no next block; gain, scale and shift are then NULL too);  stats out: [batch, N, 4] fp32, mean and 1/deviation of
+   x', mean and 1/deviation of branch (0 and 0 for a norm that is not taken), for the backward pass; may be NULL. */
+llsa_status llsa_norm_forward(const llsa_norm_plan_t *plan, const void *x, const void *branch, const float *gain_branch, const void *gate,
+                              const float *gain, const void *scale, const void *shift, void *x_out, void *y, float *stats,
+                              void *hip_stream);
+
+/*
+ * Backward pass.  x_out: x' as stored (x where there is no branch); dy: the gradient of y (NULL: y was not made); dx_out: what reaches x' by
+ * other ways, the residual stream above all (NULL: nothing); one of the two is given.  Out: dx, the gradient of x' and of x; dbranch
+ * (if branch is given); fp32, each NULL if not wanted: dgain_branch, dgain [C] and dgate, dscale, dshift [batch, C] ([1, C] if mod_stride = 0),
+ * contiguous.  dx may be dx_out's or dy's buffer, dbranch branch's.  The results are the same bits from call to call.
+ */
+llsa_status llsa_norm_backward(const llsa_norm_plan_t *plan, const void *x_out, const void *branch, const float *gain_branch,
+                               const void *gate, const float *gain, const void *scale, const float *stats, const void *dy,
+                               const void *dx_out, void *dx, void *dbranch, float *dgain_branch, float *dgate, float *dgain,
+                               float *dscale, float *dshift, void *workspace, void *hip_stream);
+
+/*
+ * Gradient of the layer glue: the adjoint of QK-Norm and RoPE as llsa_qknorm_rope_pool takes them (the pooling's is part of
+ * llsa_backward, whose dQ and dK are what comes in here).
+ *   Qpre, Kpre, gamma_q, gamma_k, cos_table, sin_table, eps: as given to llsa_qknorm_rope_pool
+ *   dQ, dK                  in : [batch, heads, N, d], gradients of Qout and Kout
+ *   dQpre, dKpre           out : [batch, heads, N, d]; may be dQ's and dK's buffers
+ *   dgamma_q, dgamma_k     out : [d] fp32
+ *   workspace                  : >= llsa_qknorm_rope_backward_bytes(plan)
+ * The results are the same bits from call to call.  Errors as llsa_qknorm_rope_pool.
+ */
+size_t llsa_qknorm_rope_backward_bytes(const llsa_plan_t *plan);
+llsa_status llsa_qknorm_rope_backward(const llsa_plan_t *plan, const void *Qpre, const void *Kpre, const float *gamma_q,
+                                      const float *gamma_k, const float *cos_table, const float *sin_table, float eps,
+                                      const void *dQ, const void *dK, void *dQpre, void *dKpre, float *dgamma_q,
+                                      float *dgamma_k, void *workspace, void *hip_stream);
+
 const char *llsa_status_string(llsa_status s);
 
 #ifdef __cplusplus

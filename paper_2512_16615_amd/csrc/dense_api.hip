@@ -1,0 +1,147 @@
+// C ABI of dense attention: host plan and launch sequences.  Nothing is allocated on the device and the host never waits.
+#include <limits.h>
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+
+#include "dense.h"
+
+namespace llsa {
+
+static size_t dense_align(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Strides as the kernels take them (bytes); false: not a layout that they take.
+static bool dense_strides(const int64_t (&st)[3], int64_t batch, int64_t heads, int64_t N, int d, int elt, DenseStrides *out) {
+    int64_t e[3] = {st[0], st[1], st[2]};
+    const int64_t n[3] = {batch, heads, N};
+    if (!e[0] && !e[1] && !e[2]) { e[2] = d; e[1] = N * d; e[0] = heads * N * d; }
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] == 1) e[i] = 0;                             // a stride nobody takes a step with
+        if (e[i] < 0 || e[i] > ((int64_t)1 << 40) || (e[i] * elt) % 16) return false;
+    }
+    *out = {e[0] * elt, e[1] * elt, e[2] * elt};
+    return true;
+}
+
+// Do rows that are written with these strides lie apart?  (Dimensions in the order of their strides, each past the one before.)
+static bool dense_apart(const DenseStrides &st, int64_t batch, int64_t heads, int64_t N, int row_bytes) {
+    std::pair<int64_t, int64_t> v[3] = {{st.batch, batch}, {st.head, heads}, {st.token, N}};
+    std::sort(v, v + 3);
+    int64_t span = row_bytes;
+    for (const auto &x : v) {
+        if (x.second == 1) continue;
+        if (x.first < span) return false;
+        span += x.first * (x.second - 1);
+    }
+    return true;
+}
+
+static llsa_status build_dense_plan(const llsa_dense_desc &d, DensePlan &p) {
+    memset(&p, 0, sizeof(p));
+    p.desc = d;
+    if (d.batch < 1 || d.heads < 1 || d.kv_heads < 1 || d.Nq < 1 || d.Nkv < 1) return LLSA_ERR_BAD_SHAPE;
+    if (d.heads % d.kv_heads) return LLSA_ERR_BAD_SHAPE;
+    if (d.dtype != LLSA_F32 && d.dtype != LLSA_BF16) return LLSA_ERR_UNSUPPORTED;
+    if (d.d != 16 && d.d != 32 && d.d != 64 && d.d != 128) return LLSA_ERR_UNSUPPORTED;
+    if ((d.causal != 0 && d.causal != 1) || (d.kernel_path != 0 && d.kernel_path != 1)) return LLSA_ERR_UNSUPPORTED;
+    p.G = d.heads / d.kv_heads;
+    // rows and keys are counted in 31 bits, groups are the grid's second dimension
+    if (d.Nq > ((int64_t)1 << 30) || d.Nkv > ((int64_t)1 << 30) || d.Nq * p.G > ((int64_t)1 << 30)) return LLSA_ERR_UNSUPPORTED;
+    if ((int64_t)d.batch * d.kv_heads > 65535) return LLSA_ERR_UNSUPPORTED;
+    p.rows = d.Nq * p.G;
+    p.elt = d.dtype == LLSA_F32 ? 4 : 2;
+    p.scale = d.sm_scale > 0.f ? d.sm_scale : (float)(1.0 / sqrt((double)d.d));
+    if (!isfinite(p.scale)) return LLSA_ERR_UNSUPPORTED;
+    if (!dense_strides(d.q_stride, d.batch, d.heads, d.Nq, d.d, p.elt, &p.q) || !dense_strides(d.k_stride, d.batch, d.kv_heads, d.Nkv, d.d, p.elt, &p.k) ||
+        !dense_strides(d.v_stride, d.batch, d.kv_heads, d.Nkv, d.d, p.elt, &p.v) || !dense_strides(d.o_stride, d.batch, d.heads, d.Nq, d.d, p.elt, &p.o))
+        return LLSA_ERR_BAD_SHAPE;
+    const int row = d.d * p.elt;
+    if (!dense_apart(p.o, d.batch, d.heads, d.Nq, row)) return LLSA_ERR_BAD_SHAPE;
+    p.grads = dense_apart(p.q, d.batch, d.heads, d.Nq, row) && dense_apart(p.k, d.batch, d.kv_heads, d.Nkv, row) &&
+              dense_apart(p.v, d.batch, d.kv_heads, d.Nkv, row);
+    p.D_off = 0;
+    p.ws_bwd = dense_align((size_t)d.batch * d.heads * d.Nq * sizeof(float));
+    return LLSA_OK;
+}
+
+static DenseArgs dense_args(const DensePlan &p, const void *Q, const void *K, const void *V, const int32_t *q_lens, const int32_t *kv_lens, float *LSE) {
+    DenseArgs a;
+    memset(&a, 0, sizeof(a));
+    a.Q = static_cast<const char *>(Q);
+    a.K = static_cast<const char *>(K);
+    a.V = static_cast<const char *>(V);
+    a.q = p.q; a.k = p.k; a.v = p.v; a.o = p.o;
+    a.q_lens = q_lens;
+    a.kv_lens = kv_lens;
+    a.LSE = LSE;
+    a.Nq = p.desc.Nq;
+    a.Nkv = p.desc.Nkv;
+    a.kv_heads = p.desc.kv_heads;
+    a.G = p.G;
+    a.div_g = FastDiv(p.G);
+    a.causal = p.desc.causal;
+    a.scale = p.scale;
+    a.scale2 = p.scale * 1.4426950408889634f;
+    return a;
+}
+
+static bool off_grid(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+template <class... P> static bool any_off_grid(size_t a, P... ptrs) { return (off_grid(ptrs, a) || ...); }
+
+}  // namespace llsa
+
+using namespace llsa;
+
+struct llsa_dense_plan_s { DensePlan p; };
+
+extern "C" {
+
+llsa_status llsa_dense_plan(const llsa_dense_desc *desc, llsa_dense_plan_t **out) {
+    if (!desc || !out) return LLSA_ERR_NULL;
+    *out = nullptr;
+    DensePlan p;
+    const llsa_status st = build_dense_plan(*desc, p);
+    if (st != LLSA_OK) return st;
+    llsa_dense_plan_s *h = new (std::nothrow) llsa_dense_plan_s;
+    if (!h) return LLSA_ERR_RUNTIME;
+    h->p = p;
+    *out = h;
+    return LLSA_OK;
+}
+
+void llsa_dense_plan_destroy(llsa_dense_plan_t *plan) { delete plan; }
+
+size_t llsa_dense_workspace_bytes(const llsa_dense_plan_t *plan, int for_backward) {
+    return !plan ? 0 : for_backward ? plan->p.ws_bwd : plan->p.ws_fwd;
+}
+
+llsa_status llsa_dense_forward(const llsa_dense_plan_t *plan, const void *Q, const void *K, const void *V, const int32_t *q_lens,
+                               const int32_t *kv_lens, void *O, float *LSE, void *workspace, void *hip_stream) {
+    if (!plan || !Q || !K || !V || !O || !LSE || (!workspace && plan->p.ws_fwd)) return LLSA_ERR_NULL;
+    if (any_off_grid(16, Q, K, V, O, LSE) || any_off_grid(4, q_lens, kv_lens) || off_grid(workspace, 256)) return LLSA_ERR_BAD_SHAPE;
+    DenseArgs a = dense_args(plan->p, Q, K, V, q_lens, kv_lens, LSE);
+    a.out = static_cast<char *>(O);
+    return launch_dense_fwd_rows(plan->p, a, (hipStream_t)hip_stream) == hipSuccess ? LLSA_OK : LLSA_ERR_RUNTIME;
+}
+
+llsa_status llsa_dense_backward(const llsa_dense_plan_t *plan, const void *Q, const void *K, const void *V, const int32_t *q_lens,
+                                const int32_t *kv_lens, const void *O, const float *LSE, const void *dO, void *dQ, void *dK,
+                                void *dV, void *workspace, void *hip_stream) {
+    if (!plan || !Q || !K || !V || !O || !LSE || !dO || !dQ || !dK || !dV || !workspace) return LLSA_ERR_NULL;
+    if (any_off_grid(16, Q, K, V, O, LSE, dO, dQ, dK, dV) || any_off_grid(4, q_lens, kv_lens) || off_grid(workspace, 256)) return LLSA_ERR_BAD_SHAPE;
+    if (!plan->p.grads) return LLSA_ERR_BAD_SHAPE;
+    DenseArgs a = dense_args(plan->p, Q, K, V, q_lens, kv_lens, const_cast<float *>(LSE));
+    a.O = static_cast<const char *>(O);
+    a.dO = static_cast<const char *>(dO);
+    a.dQ = static_cast<char *>(dQ);
+    a.dK = static_cast<char *>(dK);
+    a.dV = static_cast<char *>(dV);
+    a.D = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->p.D_off);
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (launch_dense_dq_rows(plan->p, a, s) != hipSuccess || launch_dense_dkv_rows(plan->p, a, s) != hipSuccess) return LLSA_ERR_RUNTIME;
+    return LLSA_OK;
+}
+
+}  // extern "C"

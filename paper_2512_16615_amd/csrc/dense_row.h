@@ -1,0 +1,151 @@
+// Dense attention for one row at a time: a wave, its lanes across the channels, fp32 arithmetic, keys one after the other.  Exact for every input
+// the interface allows: what a query does not see is not even read.  The tiled kernels fall back on it where a masked place holds an
+// infinity or a NaN, which a matrix instruction would multiply by 0 (NaN).
+#pragma once
+#include "dense.h"
+#include "mfma_common.h"
+
+namespace llsa {
+
+template <class T> __device__ __forceinline__ float dense_ld(const char *row, int c);
+template <> __device__ __forceinline__ float dense_ld<float>(const char *row, int c) { return reinterpret_cast<const float *>(row)[c]; }
+template <> __device__ __forceinline__ float dense_ld<__bf16>(const char *row, int c) { return (float)reinterpret_cast<const __bf16 *>(row)[c]; }
+template <class T> __device__ __forceinline__ void dense_st(char *row, int c, float x) { reinterpret_cast<T *>(row)[c] = (T)x; }
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+
+// A row's channels across the wave: lane l has channel l and, at d = 128, l + 64; the lanes beyond d have zeros.
+template <class T, int D> struct LaneRow {
+    static constexpr int n = (D + 63) / 64;
+    float x[n];
+    __device__ __forceinline__ static LaneRow load(const char *row, int lane) {
+        LaneRow r;
+#pragma unroll
+        for (int k = 0; k < n; ++k) r.x[k] = lane + 64 * k < D ? dense_ld<T>(row, lane + 64 * k) : 0.f;
+        return r;
+    }
+    __device__ __forceinline__ static LaneRow zero() {
+        LaneRow r;
+#pragma unroll
+        for (int k = 0; k < n; ++k) r.x[k] = 0.f;
+        return r;
+    }
+    __device__ __forceinline__ void store(char *row, int lane) const {
+#pragma unroll
+        for (int k = 0; k < n; ++k)
+            if (lane + 64 * k < D) dense_st<T>(row, lane + 64 * k, x[k]);
+    }
+    __device__ __forceinline__ void scale(float f) {
+#pragma unroll
+        for (int k = 0; k < n; ++k) x[k] *= f;
+    }
+    __device__ __forceinline__ void add(float f, const LaneRow &o) {
+#pragma unroll
+        for (int k = 0; k < n; ++k) x[k] = fmaf(f, o.x[k], x[k]);
+    }
+    __device__ __forceinline__ float dot(const LaneRow &o) const {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < n; ++k) s = fmaf(x[k], o.x[k], s);
+        return wave_sum(s);
+    }
+};
+
+// one group (batch entry and key head) of the problem
+struct DenseGroup {
+    const char *Q, *K, *V, *O, *dO;
+    char *out, *dQ, *dK, *dV;
+    float *LSE;                     // of the group's first head
+    int nq, nk;                     // lengths
+    __device__ __forceinline__ DenseGroup(const DenseArgs &a, int group) {
+        const int b = group / a.kv_heads, h = group - b * a.kv_heads;
+        const int64_t oq = b * a.q.batch + (int64_t)h * a.G * a.q.head, oo = b * a.o.batch + (int64_t)h * a.G * a.o.head;
+        const int64_t ok = b * a.k.batch + h * a.k.head, ov = b * a.v.batch + h * a.v.head;
+        Q = a.Q + oq;
+        K = a.K + ok;
+        V = a.V + ov;
+        O = a.O + oo;
+        dO = a.dO + oo;
+        out = a.out + oo;
+        dQ = a.dQ + oq;
+        dK = a.dK + ok;
+        dV = a.dV + ov;
+        LSE = a.LSE + ((int64_t)b * a.kv_heads + h) * a.G * a.Nq;
+        nq = a.q_lens ? max(0, min(a.q_lens[b], (int)a.Nq)) : (int)a.Nq;
+        nk = a.kv_lens ? max(0, min(a.kv_lens[b], (int)a.Nkv)) : (int)a.Nkv;
+    }
+    // keys that query i sees: 0 .. seen(i) - 1
+    __device__ __forceinline__ int seen(const DenseArgs &a, int i) const {
+        return i >= nq ? 0 : a.causal ? max(0, min(nk, i + nk - nq + 1)) : nk;
+    }
+    // first query that sees key j (nq: none does)
+    __device__ __forceinline__ int first_query(const DenseArgs &a, int j) const { return j >= nk ? nq : a.causal ? min(nq, max(0, j - nk + nq)) : 0; }
+};
+
+template <class T, int D> __device__ __forceinline__ void dense_row_forward(const DenseArgs &a, const DenseGroup &p, int i, int g, int lane) {
+    using Row = LaneRow<T, D>;
+    const Row q = Row::load(p.Q + g * a.q.head + i * a.q.token, lane);
+    const int n = p.seen(a, i);
+    Row acc = Row::zero();
+    float m = -INFINITY, l = 0.f;
+    for (int j = 0; j < n; ++j) {
+        const float s = q.dot(Row::load(p.K + j * a.k.token, lane)) * a.scale;
+        const float m2 = fmaxf(m, s);
+        if (m2 > m) {                                        // the sums so far, relative to the new maximum
+            const float f = __expf(m - m2);
+            l *= f;
+            acc.scale(f);
+            m = m2;
+        }
+        const float e = s == -INFINITY && m == -INFINITY ? 0.f : __expf(s - m);
+        l += e;
+        acc.add(e, Row::load(p.V + j * a.v.token, lane));
+    }
+    if (n > 0) acc.scale(1.f / l);
+    acc.store(p.out + g * a.o.head + i * a.o.token, lane);
+    if (lane == 0) p.LSE[(int64_t)g * a.Nq + i] = n > 0 ? m + __logf(l) : -INFINITY;
+}
+
+// D of the row comes as an argument: both passes of the backward use the same one
+template <class T, int D> __device__ __forceinline__ void dense_row_dq(const DenseArgs &a, const DenseGroup &p, int i, int g, float delta, int lane) {
+    using Row = LaneRow<T, D>;
+    Row acc = Row::zero();
+    const int n = p.seen(a, i);
+    if (n > 0) {
+        const Row q = Row::load(p.Q + g * a.q.head + i * a.q.token, lane), go = Row::load(p.dO + g * a.o.head + i * a.o.token, lane);
+        const float lse = p.LSE[(int64_t)g * a.Nq + i];
+        for (int j = 0; j < n; ++j) {
+            const Row k = Row::load(p.K + j * a.k.token, lane);
+            const float e = __expf(q.dot(k) * a.scale - lse);
+            acc.add(e * (go.dot(Row::load(p.V + j * a.v.token, lane)) - delta), k);
+        }
+        acc.scale(a.scale);
+    }
+    acc.store(p.dQ + g * a.q.head + i * a.q.token, lane);
+}
+
+// delta: D of the group's rows (row i * G + g)
+template <class T, int D> __device__ __forceinline__ void dense_row_dkv(const DenseArgs &a, const DenseGroup &p, int j, const float *delta, int lane) {
+    using Row = LaneRow<T, D>;
+    Row dk = Row::zero(), dv = Row::zero();
+    const int first = p.first_query(a, j);
+    if (first < p.nq) {
+        const Row k = Row::load(p.K + j * a.k.token, lane), v = Row::load(p.V + j * a.v.token, lane);
+        for (int i = first; i < p.nq; ++i)
+            for (int g = 0; g < a.G; ++g) {
+                const Row q = Row::load(p.Q + g * a.q.head + i * a.q.token, lane), go = Row::load(p.dO + g * a.o.head + i * a.o.token, lane);
+                const float e = __expf(q.dot(k) * a.scale - p.LSE[(int64_t)g * a.Nq + i]);
+                dv.add(e, go);
+                dk.add(e * (go.dot(v) - delta[(int64_t)i * a.G + g]), q);
+            }
+        dk.scale(a.scale);
+    }
+    dk.store(p.dK + j * a.k.token, lane);
+    dv.store(p.dV + j * a.v.token, lane);
+}
+
+}  // namespace llsa

@@ -398,6 +398,22 @@ llsa_status llsa_qknorm_rope_pool(const llsa_plan_t *plan, const void *Qpre, con
     return LLSA_OK;
 }
 
+size_t llsa_qknorm_rope_backward_bytes(const llsa_plan_t *plan) { return plan ? glue_backward_bytes(plan->p) : 0; }
+
+llsa_status llsa_qknorm_rope_backward(const llsa_plan_t *plan, const void *Qpre, const void *Kpre, const float *gamma_q,
+                                      const float *gamma_k, const float *cos_table, const float *sin_table, float eps,
+                                      const void *dQ, const void *dK, void *dQpre, void *dKpre, float *dgamma_q,
+                                      float *dgamma_k, void *workspace, void *hip_stream) {
+    if (!plan || !Qpre || !Kpre || !gamma_q || !gamma_k || !cos_table || !sin_table || !dQ || !dK || !dQpre || !dKpre || !dgamma_q ||
+        !dgamma_k || !workspace)
+        return LLSA_ERR_NULL;
+    if (any_misaligned16(Qpre, Kpre, dQ, dK, dQpre, dKpre, cos_table, sin_table) || misaligned(workspace, 256)) return LLSA_ERR_BAD_SHAPE;
+    if (!(eps >= 0.f)) return LLSA_ERR_BAD_SHAPE;
+    LLSA_TRY(launch_glue_backward(plan->p, Qpre, Kpre, gamma_q, gamma_k, cos_table, sin_table, eps, dQ, dK, dQpre, dKpre, dgamma_q,
+                                  dgamma_k, workspace, (hipStream_t)hip_stream));
+    return LLSA_OK;
+}
+
 static llsa_status forward_impl(const llsa_plan_t *plan, const void *Q, const void *K, const void *V, void *O, float *LSE,
                                 int32_t *indices, void *workspace, void *hip_stream, bool pool) {
     const Plan &p = plan->p;

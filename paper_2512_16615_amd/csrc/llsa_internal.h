@@ -111,6 +111,11 @@ hipError_t launch_pool(const Plan &p, const void *Q, const void *K, const void *
 hipError_t launch_qknorm_rope_pool(const Plan &p, const void *Qpre, const void *Kpre, const void *V,
                                    const float *gamma_q, const float *gamma_k, const float *cos_t, const float *sin_t,
                                    float eps, void *Qout, void *Kout, void *ws, hipStream_t s);
+// the gradient of that glue (glue_backward.hip)
+size_t glue_backward_bytes(const Plan &p);
+hipError_t launch_glue_backward(const Plan &p, const void *Qpre, const void *Kpre, const float *gamma_q, const float *gamma_k, const float *cos_t,
+                                const float *sin_t, float eps, const void *dQ, const void *dK, void *dQpre, void *dKpre, float *dgamma_q, float *dgamma_k,
+                                void *ws, hipStream_t s);
 hipError_t launch_select(const Plan &p, int l, const void *ws, const int32_t *parent, int32_t *out, hipStream_t s);
 hipError_t launch_csc(const Plan &p, int top_level, const int32_t *I, void *ws, hipStream_t s);  // levels 0..top_level
 bool csc_small_args(const Plan &p, int top_level, const int32_t *I, void *ws, CscSmall *a);   // false (and none): too many rows

@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libllsa.so")
 _lib = None
 
 F32, BF16 = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
 
 
 class LlsaError(RuntimeError):
@@ -30,12 +31,28 @@ class _Desc(ctypes.Structure):
                 ("bwd_repool", ctypes.c_int32), ("kernel_path", ctypes.c_int32), ("single_stream", ctypes.c_int32)]
 
 
+class _DenseDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("Nq", ctypes.c_int64), ("Nkv", ctypes.c_int64), ("sm_scale", ctypes.c_float), ("dtype", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("kernel_path", ctypes.c_int32), ("q_stride", ctypes.c_int64 * 3),
+                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3), ("o_stride", ctypes.c_int64 * 3)]
+
+
+class _NormDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("C", ctypes.c_int32), ("N", ctypes.c_int64), ("kind", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("dtype", ctypes.c_int32),
+                ("mod_dtype", ctypes.c_int32), ("mod_stride", ctypes.c_int64)]
+
+
 EXPORTS = ["llsa_plan", "llsa_plan_destroy", "llsa_plan_workspace_bytes", "llsa_plan_indices_bytes",
            "llsa_plan_level_info", "llsa_plan_pyramid_info", "llsa_plan_csc_info", "llsa_forward", "llsa_backward",
            "llsa_pool", "llsa_select_level", "llsa_attention", "llsa_index_transpose", "llsa_reorder", "llsa_status_string",
            "llsa_stage_count", "llsa_stage_name", "llsa_stage_timing_begin", "llsa_stage_timing_end",
            "llsa_static_workspace_bytes", "llsa_forward_static", "llsa_qknorm_rope_pool", "llsa_forward_pooled",
-           "llsa_kv_backward_mask_bytes", "llsa_kv_backward_level0", "llsa_calibrate_mfma", "llsa_calibrate_copy"]
+           "llsa_kv_backward_mask_bytes", "llsa_kv_backward_level0", "llsa_calibrate_mfma", "llsa_calibrate_copy",
+           "llsa_dense_plan", "llsa_dense_plan_destroy", "llsa_dense_workspace_bytes", "llsa_dense_forward", "llsa_dense_backward",
+           "llsa_norm_plan", "llsa_norm_plan_destroy", "llsa_norm_workspace_bytes", "llsa_norm_forward", "llsa_norm_backward",
+           "llsa_qknorm_rope_backward_bytes", "llsa_qknorm_rope_backward"]
 
 
 def load():
@@ -99,6 +116,30 @@ def load():
     lib.llsa_stage_timing_begin.restype = ctypes.c_int
     lib.llsa_stage_timing_end.argtypes = [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i32)]
     lib.llsa_stage_timing_end.restype = ctypes.c_int
+    lib.llsa_dense_plan.argtypes = [ctypes.POINTER(_DenseDesc), ctypes.POINTER(vp)]
+    lib.llsa_dense_plan.restype = ctypes.c_int
+    lib.llsa_dense_plan_destroy.argtypes = [vp]
+    lib.llsa_dense_plan_destroy.restype = None
+    lib.llsa_dense_workspace_bytes.argtypes = [vp, ctypes.c_int]
+    lib.llsa_dense_workspace_bytes.restype = sz
+    lib.llsa_dense_forward.argtypes = [vp] * 10
+    lib.llsa_dense_forward.restype = ctypes.c_int
+    lib.llsa_dense_backward.argtypes = [vp] * 14
+    lib.llsa_dense_backward.restype = ctypes.c_int
+    lib.llsa_norm_plan.argtypes = [ctypes.POINTER(_NormDesc), ctypes.POINTER(vp)]
+    lib.llsa_norm_plan.restype = ctypes.c_int
+    lib.llsa_norm_plan_destroy.argtypes = [vp]
+    lib.llsa_norm_plan_destroy.restype = None
+    lib.llsa_norm_workspace_bytes.argtypes = [vp]
+    lib.llsa_norm_workspace_bytes.restype = sz
+    lib.llsa_norm_forward.argtypes = [vp] * 12
+    lib.llsa_norm_forward.restype = ctypes.c_int
+    lib.llsa_norm_backward.argtypes = [vp] * 19
+    lib.llsa_norm_backward.restype = ctypes.c_int
+    lib.llsa_qknorm_rope_backward_bytes.argtypes = [vp]
+    lib.llsa_qknorm_rope_backward_bytes.restype = sz
+    lib.llsa_qknorm_rope_backward.argtypes = [vp] * 7 + [ctypes.c_float] + [vp] * 8
+    lib.llsa_qknorm_rope_backward.restype = ctypes.c_int
     lib.llsa_status_string.argtypes = [ctypes.c_int]
     lib.llsa_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -186,6 +227,10 @@ class Plan:
     def alloc_indices(self, device="cuda") -> torch.Tensor:
         return torch.empty(self.indices_bytes() // 4, dtype=torch.int32, device=device)
 
+    def alloc_glue_workspace(self, device="cuda") -> torch.Tensor:
+        """Workspace of ``qknorm_rope_backward``."""
+        return torch.empty(load().llsa_qknorm_rope_backward_bytes(self._h), dtype=torch.uint8, device=device)
+
     def level_indices(self, indices: torch.Tensor, l: int) -> torch.Tensor:
         """View of I^(l) inside ``indices``: ``[batch, heads, rows, K_l]``."""
         li = self.levels[l]
@@ -244,6 +289,51 @@ def qknorm_rope_pool(p: Plan, Qpre, Kpre, V, gamma_q, gamma_k, cos_table, sin_ta
                                         _ptr(cos_table), _ptr(sin_table), ctypes.c_float(eps), _ptr(Qout), _ptr(Kout),
                                         _ptr(workspace), _stream()), "llsa_qknorm_rope_pool")
     return Qout, Kout, workspace
+
+
+def _chk_here(t: torch.Tensor, name: str):
+    """The kernels run on the current device's current stream."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise LlsaError(f"{name}: expected a tensor on the current device, got one on {t.device}")
+
+
+def _chk_vec(t: torch.Tensor, name: str, dtype, shape, last_only=False):
+    """A tensor of exactly this type and shape; contiguous, or with contiguous rows."""
+    _chk_here(t, name)
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise LlsaError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not (t.is_contiguous() or last_only and t.stride(-1) == 1):
+        raise LlsaError(f"{name}: expected a contiguous tensor, got strides {t.stride()}")
+
+
+def _chk_ws(t: torch.Tensor | None, name: str, nbytes: int):
+    if t is None:
+        return
+    _chk_here(t, name)
+    if t.numel() * t.element_size() < nbytes or not t.is_contiguous():
+        raise LlsaError(f"{name}: {nbytes} contiguous bytes are needed")
+
+
+def qknorm_rope_backward(p: Plan, Qpre, Kpre, gamma_q, gamma_k, cos_table, sin_table, dQ, dK, eps=1e-6, dQpre=None, dKpre=None,
+                         dgamma_q=None, dgamma_k=None, workspace=None):
+    """``llsa_qknorm_rope_backward``: returns ``(dQpre, dKpre, dgamma_q, dgamma_k)`` from the gradients ``dQ``, ``dK`` of the tensors that
+    ``qknorm_rope_pool`` made (as ``backward`` returns them).  ``dQpre`` may be ``dQ``, ``dKpre`` ``dK``."""
+    dQpre = torch.empty_like(Qpre) if dQpre is None else dQpre
+    dKpre = torch.empty_like(Kpre) if dKpre is None else dKpre
+    for t, n in ((Qpre, "Qpre"), (Kpre, "Kpre"), (dQ, "dQ"), (dK, "dK"), (dQpre, "dQpre"), (dKpre, "dKpre")):
+        _chk_here(t, n)
+        _chk_tensor(p, t, n)
+    dgamma_q = torch.empty(p.d, dtype=torch.float32, device=Qpre.device) if dgamma_q is None else dgamma_q
+    dgamma_k = torch.empty(p.d, dtype=torch.float32, device=Qpre.device) if dgamma_k is None else dgamma_k
+    for t, shape, n in ((gamma_q, (p.d,), "gamma_q"), (gamma_k, (p.d,), "gamma_k"), (dgamma_q, (p.d,), "dgamma_q"), (dgamma_k, (p.d,), "dgamma_k"),
+                        (cos_table, (p.N, p.d // 2), "cos_table"), (sin_table, (p.N, p.d // 2), "sin_table")):
+        _chk_vec(t, n, torch.float32, shape)
+    workspace = p.alloc_glue_workspace(Qpre.device) if workspace is None else workspace
+    _chk_ws(workspace, "workspace", load().llsa_qknorm_rope_backward_bytes(p._h))
+    _check(load().llsa_qknorm_rope_backward(p._h, _ptr(Qpre), _ptr(Kpre), _ptr(gamma_q), _ptr(gamma_k), _ptr(cos_table), _ptr(sin_table),
+                                            ctypes.c_float(eps), _ptr(dQ), _ptr(dK), _ptr(dQpre), _ptr(dKpre), _ptr(dgamma_q),
+                                            _ptr(dgamma_k), _ptr(workspace), _stream()), "llsa_qknorm_rope_backward")
+    return dQpre, dKpre, dgamma_q, dgamma_k
 
 
 def forward_pooled(p: Plan, Q, K, V, workspace, O=None, LSE=None, indices=None):
@@ -343,6 +433,185 @@ def reorder(x: torch.Tensor, inverse: bool = False, out: torch.Tensor | None = N
     out = torch.empty_like(x) if out is None else out
     _check(load().llsa_reorder(x.numel() // (N * d), N, d, dtype, int(inverse), _ptr(x), _ptr(out), _stream()), "llsa_reorder")
     return out
+
+
+# ---- dense attention
+
+class DensePlan:
+    """``llsa_dense_plan``: attention over all keys (host only).  Strides are in elements, ``(batch, head, token)``, as the first three of
+    ``tensor.stride()`` of a ``[batch, heads, N, d]`` view; None: contiguous."""
+
+    def __init__(self, batch, heads, Nq, Nkv, d, kv_heads=None, sm_scale=0.0, dtype=BF16, causal=False, kernel_path=0, q_stride=None,
+                 k_stride=None, v_stride=None, o_stride=None):
+        lib = load()
+        kv_heads = heads if kv_heads is None else kv_heads
+        strides = [tuple(s) if s is not None else (0, 0, 0) for s in (q_stride, k_stride, v_stride, o_stride)]
+        if any(len(s) != 3 for s in strides):
+            raise LlsaError("llsa_dense_plan: strides are (batch, head, token)")
+        self.desc = _DenseDesc(batch, heads, kv_heads, d, Nq, Nkv, sm_scale, dtype, int(causal), kernel_path,
+                               *((ctypes.c_int64 * 3)(*s) for s in strides))
+        h = ctypes.c_void_p()
+        st = lib.llsa_dense_plan(ctypes.byref(self.desc), ctypes.byref(h))
+        self._h = h if st == 0 else None
+        _check(st, "llsa_dense_plan")
+        self.batch, self.heads, self.kv_heads, self.Nq, self.Nkv, self.d = batch, heads, kv_heads, Nq, Nkv, d
+        self.torch_dtype = torch.float32 if dtype == F32 else torch.bfloat16
+        self._q, self._kv = torch.Size((batch, heads, Nq, d)), torch.Size((batch, kv_heads, Nkv, d))
+        self._strides = {}
+        for name, st, size in zip("qkvo", strides, (self._q, self._kv, self._kv, self._q)):
+            if not any(st):
+                st = (size[1] * size[2] * d, size[2] * d, d)
+            self._strides[name] = (*st, 1)
+        self._workspace_bytes = tuple(lib.llsa_dense_workspace_bytes(self._h, i) for i in (0, 1))
+
+    def __del__(self):
+        if getattr(self, "_h", None) is not None and _lib is not None:
+            _lib.llsa_dense_plan_destroy(self._h)
+            self._h = None
+
+    def workspace_bytes(self, for_backward: bool) -> int:
+        return self._workspace_bytes[bool(for_backward)]
+
+    def alloc_workspace(self, for_backward: bool, device="cuda") -> torch.Tensor:
+        """A workspace for the forward or for the backward; the backward's serves both."""
+        n = self.workspace_bytes(False)
+        return torch.empty(max(n, self.workspace_bytes(True) if for_backward else n, 256), dtype=torch.uint8, device=device)
+
+    def empty(self, which: str, device="cuda") -> torch.Tensor:
+        """An uninitialised tensor with the plan's strides: ``"q"`` (Q, dQ), ``"k"``, ``"v"`` or ``"o"`` (O, dO)."""
+        size, st = (self._q if which in "qo" else self._kv), self._strides[which]
+        if any(s == 0 and n > 1 for n, s in zip(size, st)):
+            raise LlsaError(f"{which}: rows of a tensor to be written would overlap")
+        return torch.empty_strided(size, st, dtype=self.torch_dtype, device=device)
+
+    def _check_tensor(self, t: torch.Tensor, name: str, which: str):
+        size = self._q if which in "qo" else self._kv
+        if t.dtype != self.torch_dtype or t.shape != size or any(n > 1 and a != b for n, a, b in zip(size, t.stride(), self._strides[which])):
+            raise LlsaError(f"{name}: expected {self.torch_dtype} {tuple(size)} with strides {self._strides[which]}, got {t.dtype} "
+                            f"{tuple(t.shape)} with strides {t.stride()}")
+        _chk_here(t, name)
+
+    def _check_lens(self, q_lens, kv_lens):
+        for t, n in ((q_lens, "q_lens"), (kv_lens, "kv_lens")):
+            if t is not None:
+                _chk_vec(t, n, torch.int32, (self.batch,))
+
+
+def dense_forward(p: DensePlan, Q, K, V, q_lens=None, kv_lens=None, O=None, LSE=None, workspace=None):
+    """``llsa_dense_forward``: returns ``(O, LSE)``.  ``q_lens``, ``kv_lens``: ``[batch]`` int32 on the device."""
+    p._check_tensor(Q, "Q", "q")
+    p._check_tensor(K, "K", "k")
+    p._check_tensor(V, "V", "v")
+    p._check_lens(q_lens, kv_lens)
+    O = p.empty("o", Q.device) if O is None else O
+    p._check_tensor(O, "O", "o")
+    LSE = torch.empty(p.batch, p.heads, p.Nq, dtype=torch.float32, device=Q.device) if LSE is None else LSE
+    _chk_vec(LSE, "LSE", torch.float32, (p.batch, p.heads, p.Nq))
+    need = p._workspace_bytes[0]
+    workspace = p.alloc_workspace(False, Q.device) if workspace is None and need else workspace
+    _chk_ws(workspace, "workspace", need)
+    _check(load().llsa_dense_forward(p._h, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_lens), _ptr(kv_lens), _ptr(O), _ptr(LSE), _ptr(workspace),
+                                     _stream()), "llsa_dense_forward")
+    return O, LSE
+
+
+def dense_backward(p: DensePlan, Q, K, V, O, LSE, dO, q_lens=None, kv_lens=None, dQ=None, dK=None, dV=None, workspace=None):
+    """``llsa_dense_backward``: returns ``(dQ, dK, dV)``, with the strides of Q, K and V."""
+    dQ = p.empty("q", Q.device) if dQ is None else dQ
+    dK = p.empty("k", Q.device) if dK is None else dK
+    dV = p.empty("v", Q.device) if dV is None else dV
+    for t, n, which in ((Q, "Q", "q"), (K, "K", "k"), (V, "V", "v"), (O, "O", "o"), (dO, "dO", "o"), (dQ, "dQ", "q"), (dK, "dK", "k"), (dV, "dV", "v")):
+        p._check_tensor(t, n, which)
+    p._check_lens(q_lens, kv_lens)
+    _chk_vec(LSE, "LSE", torch.float32, (p.batch, p.heads, p.Nq))
+    workspace = p.alloc_workspace(True, Q.device) if workspace is None else workspace
+    _chk_ws(workspace, "workspace", p._workspace_bytes[1])
+    _check(load().llsa_dense_backward(p._h, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_lens), _ptr(kv_lens), _ptr(O), _ptr(LSE), _ptr(dO), _ptr(dQ),
+                                      _ptr(dK), _ptr(dV), _ptr(workspace), _stream()), "llsa_dense_backward")
+    return dQ, dK, dV
+
+
+# ---- the norms between two blocks
+
+class NormPlan:
+    """``llsa_norm_plan`` (host only).  ``mod_stride``: elements between the rows of ``gate``, ``scale`` and ``shift`` for two batch entries; None:
+    ``C``; 0: they have one row, ``[1, C]``, for all batch entries."""
+
+    def __init__(self, batch, N, C, kind=NORM_RMS, eps=1e-6, residual_scale=1.0, dtype=BF16, mod_dtype=F32, mod_stride=None):
+        lib = load()
+        mod_stride = C if mod_stride is None else mod_stride
+        self.desc = _NormDesc(batch, C, N, kind, eps, residual_scale, dtype, mod_dtype, mod_stride)
+        h = ctypes.c_void_p()
+        st = lib.llsa_norm_plan(ctypes.byref(self.desc), ctypes.byref(h))
+        self._h = h if st == 0 else None
+        _check(st, "llsa_norm_plan")
+        self.batch, self.N, self.C, self.mod_stride = batch, N, C, mod_stride
+        self.torch_dtype = torch.float32 if dtype == F32 else torch.bfloat16
+        self.mod_torch_dtype = torch.float32 if mod_dtype == F32 else torch.bfloat16
+        self._mod_rows = batch if mod_stride else 1
+        self._workspace_bytes = lib.llsa_norm_workspace_bytes(self._h)
+
+    def __del__(self):
+        if getattr(self, "_h", None) is not None and _lib is not None:
+            _lib.llsa_norm_plan_destroy(self._h)
+            self._h = None
+
+    def workspace_bytes(self) -> int:
+        return self._workspace_bytes
+
+    def alloc_workspace(self, device="cuda") -> torch.Tensor:
+        return torch.empty(self._workspace_bytes, dtype=torch.uint8, device=device)
+
+    def _check(self, rows=(), vecs=(), mods=()):
+        for t, n in rows:
+            if t is not None:
+                _chk_vec(t, n, self.torch_dtype, (self.batch, self.N, self.C))
+        for t, n in vecs:
+            if t is not None:
+                _chk_vec(t, n, torch.float32, (self.C,))
+        for t, n in mods:
+            if t is not None:
+                _chk_vec(t, n, self.mod_torch_dtype, (self._mod_rows, self.C), last_only=True)
+                if self._mod_rows > 1 and t.stride(0) != self.mod_stride:
+                    raise LlsaError(f"{n}: expected rows {self.mod_stride} elements apart, got strides {t.stride()}")
+
+
+def norm_forward(p: NormPlan, x, branch=None, gain_branch=None, gate=None, gain=None, scale=None, shift=None, x_out=None, y=None, stats=None,
+                 want_y=True):
+    """``llsa_norm_forward``: returns ``(x_out, y, stats)``; ``x_out`` is ``x`` where there is no branch, ``y`` None if not wanted."""
+    if branch is None:
+        x_out = None
+    else:
+        x_out = torch.empty_like(x) if x_out is None else x_out
+    y = None if not want_y else torch.empty_like(x) if y is None else y
+    p._check(((x, "x"), (branch, "branch"), (x_out, "x_out"), (y, "y")), ((gain_branch, "gain_branch"), (gain, "gain")),
+             ((gate, "gate"), (scale, "scale"), (shift, "shift")))
+    stats = torch.empty(p.batch, p.N, 4, dtype=torch.float32, device=x.device) if stats is None else stats
+    _chk_vec(stats, "stats", torch.float32, (p.batch, p.N, 4))
+    _check(load().llsa_norm_forward(p._h, _ptr(x), _ptr(branch), _ptr(gain_branch), _ptr(gate), _ptr(gain), _ptr(scale), _ptr(shift), _ptr(x_out),
+                                    _ptr(y), _ptr(stats), _stream()), "llsa_norm_forward")
+    return x if branch is None else x_out, y, stats
+
+
+def norm_backward(p: NormPlan, x_out, dy, stats, branch=None, gain_branch=None, gate=None, gain=None, scale=None, shift=None, dx_out=None, dx=None,
+                  dbranch=None, workspace=None):
+    """``llsa_norm_backward``: a dict with ``dx``, ``dbranch`` and the fp32 gradients of those of ``gain_branch``, ``gate``, ``gain``, ``scale``, ``shift``
+    (whose values are not needed) that are given.  ``dx`` may be ``dy`` or ``dx_out``, ``dbranch`` may be ``branch``."""
+    dx = torch.empty_like(x_out) if dx is None else dx
+    dbranch = None if branch is None else torch.empty_like(branch) if dbranch is None else dbranch
+    p._check(((x_out, "x_out"), (dy, "dy"), (branch, "branch"), (dx_out, "dx_out"), (dx, "dx"), (dbranch, "dbranch")),
+             ((gain_branch, "gain_branch"), (gain, "gain")), ((gate, "gate"), (scale, "scale"), (shift, "shift")))
+    _chk_vec(stats, "stats", torch.float32, (p.batch, p.N, 4))
+    new = lambda t, *shape: None if t is None else torch.empty(*shape, dtype=torch.float32, device=x_out.device)
+    out = {"dx": dx, "dbranch": dbranch, "dgain_branch": new(gain_branch, p.C), "dgate": new(gate, p._mod_rows, p.C), "dgain": new(gain, p.C),
+           "dscale": new(scale, p._mod_rows, p.C), "dshift": new(shift, p._mod_rows, p.C)}
+    if workspace is None and any(out[n] is not None for n in ("dgain_branch", "dgate", "dgain", "dscale", "dshift")):
+        workspace = p.alloc_workspace(x_out.device)
+    _chk_ws(workspace, "workspace", p._workspace_bytes)
+    _check(load().llsa_norm_backward(p._h, _ptr(x_out), _ptr(branch), _ptr(gain_branch), _ptr(gate), _ptr(gain), _ptr(scale), _ptr(stats), _ptr(dy),
+                                     _ptr(dx_out), _ptr(dx), _ptr(dbranch), *(_ptr(out[n]) for n in ("dgain_branch", "dgate", "dgain", "dscale", "dshift")),
+                                     _ptr(workspace), _stream()), "llsa_norm_backward")
+    return {n: t for n, t in out.items() if t is not None}
 
 
 def measured_peaks(mfma_iters: int = 20000, copy_bytes: int = 1 << 30, reps: int = 5) -> dict:

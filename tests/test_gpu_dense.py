@@ -1,0 +1,246 @@
+"""Dense attention, forward and backward, against 64 bits (tests/operators_reference.py holds the forms and derives the bounds)."""
+import math
+
+import pytest
+import torch
+
+from paper_2512_16615_amd import llsa
+from tests import operators_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+def _case(dtype, batch, heads, kv_heads, Nq, Nkv, d, causal=False, lens=None, layout="heads", sm_scale=0.0, path=0):
+    return dict(dtype=dtype, batch=batch, heads=heads, kv_heads=kv_heads, Nq=Nq, Nkv=Nkv, d=d, causal=causal, lens=lens, layout=layout, sm_scale=sm_scale, path=path)
+
+
+def _id(c):
+    lens = "" if c["lens"] is None else "-" + ("q" if c["lens"][0] else "") + "kv" + "_".join(map(str, c["lens"][1] or c["lens"][0]))
+    return (f"{c['dtype']}-{c['batch']}x{c['heads']}_{c['kv_heads']}-{c['Nq']}x{c['Nkv']}-d{c['d']}{'-causal' if c['causal'] else ''}{lens}-{c['layout']}"
+            f"{'-rows' if c['path'] else ''}{'-scale' if c['sm_scale'] else ''}")
+
+
+def _tensor(c, heads, N, gen, k=1.0):
+    """[batch, heads, N, d] as a view: heads first, tokens first, or a piece of a wider projection (with what lies between poisoned)."""
+    b, d = c["batch"], c["d"]
+    x = k * torch.randn(b, heads, N, d, generator=gen)
+    x = x.to(torch.bfloat16 if c["dtype"] == "bf16" else torch.float32).cuda()
+    if c["layout"] == "tokens":
+        return x.transpose(1, 2).contiguous().transpose(1, 2)
+    if c["layout"] == "piece":
+        wide = torch.full((b, N, heads + 1, d), math.nan, dtype=x.dtype, device="cuda")
+        wide[:, :, :heads] = x.transpose(1, 2)
+        return wide[:, :, :heads].transpose(1, 2)
+    return x
+
+
+def _inputs(c, seed=0, k=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    Q, dO = (_tensor(c, c["heads"], c["Nq"], gen, s) for s in (k, 1.0))
+    K, V = (_tensor(c, c["kv_heads"], c["Nkv"], gen, s) for s in (k, 1.0))
+    lens = [None if c["lens"] is None or v is None else torch.tensor(v, dtype=torch.int32, device="cuda") for v in (c["lens"] or (None, None))]
+    return Q, K, V, dO, *lens
+
+
+def _plan(c, Q, K, V, O=None):
+    st = lambda t: t.stride()[:3]
+    return llsa.DensePlan(c["batch"], c["heads"], c["Nq"], c["Nkv"], c["d"], kv_heads=c["kv_heads"], causal=c["causal"], sm_scale=c["sm_scale"],
+                          dtype=llsa.BF16 if c["dtype"] == "bf16" else llsa.F32, kernel_path=c["path"], q_stride=st(Q), k_stride=st(K), v_stride=st(V),
+                          o_stride=st(Q if O is None else O))
+
+
+def _poisoned(p, which):
+    """A tensor of the plan's layout whose every element, also between the rows, is a NaN."""
+    st, size = p._strides[which], p._q if which in "qo" else p._kv
+    n = 1 + sum((a - 1) * s for a, s in zip(size, st))
+    store = torch.full((n,), math.nan, dtype=p.torch_dtype, device="cuda")
+    return store.as_strided(size, st), store
+
+
+def _run(c, Q, K, V, dO, ql, kl, workspace=None):
+    p = _plan(c, Q, K, V)
+    O = _poisoned(p, "o")[0]
+    LSE = torch.full((c["batch"], c["heads"], c["Nq"]), math.nan, device="cuda")
+    ws = p.alloc_workspace(True) if workspace is None else workspace
+    ws.fill_(0xff)
+    llsa.dense_forward(p, Q, K, V, ql, kl, O, LSE, ws)
+    ws.fill_(0xff)
+    grads = {n: _poisoned(p, w) for n, w in (("dQ", "q"), ("dK", "k"), ("dV", "v"))}
+    llsa.dense_backward(p, Q, K, V, O, LSE, dO, ql, kl, *(t for t, _ in grads.values()), ws)
+    torch.cuda.synchronize()
+    out = {"O": O, "LSE": LSE} | {n: t for n, (t, _) in grads.items()}
+    for n, (t, store) in grads.items():              # what lies between the rows is left alone
+        assert int((~torch.isnan(store)).sum()) == t.numel() - int(torch.isnan(t).sum()), n
+    return out
+
+
+def _check(c, got, Q, K, V, dO, ql, kl, names=("O", "LSE", "dQ", "dK", "dV")):
+    want, tol = R.dense(Q, K, V, dO, c["causal"], ql, kl, c["sm_scale"] or None, torch.bfloat16 if c["dtype"] == "bf16" else torch.float32)
+    worst = {}
+    for n in names:
+        g, w = got[n].double(), want[n]
+        fine = torch.isfinite(w)
+        assert torch.equal(fine, torch.isfinite(g)), f"{n}: other places are finite"
+        assert torch.equal(g[~fine].isnan(), w[~fine].isnan()) and torch.equal(g[~fine].nan_to_num(0.0), w[~fine].nan_to_num(0.0)), f"{n}: values that are not finite"
+        err = (g - w).abs()[fine]
+        over = err / tol[n][fine]
+        worst[n] = float(over.max()) if over.numel() else 0.0
+        assert worst[n] <= 1.0, f"{n}: {worst[n]:.2f} of the bound; largest error {float(err.max()):.3e} of {float(w[fine].abs().max()):.3e}"
+    print({n: round(v, 3) for n, v in worst.items()}, flush=True)
+
+
+CASES = [
+    # one token, one key; a few of each
+    _case("bf16", 1, 1, 1, 1, 1, 64), _case("f32", 2, 2, 1, 1, 1, 16), _case("bf16", 1, 2, 2, 2, 3, 128), _case("f32", 1, 3, 1, 5, 2, 32),
+    # around the tiles' sizes
+    *[_case("bf16", 1, 2, 2, n, n, 64) for n in (31, 32, 33, 63, 64, 65, 127, 128, 129, 257)],
+    *[_case("bf16", 1, 1, 1, n, m, 128) for n, m in ((33, 95), (64, 96), (129, 63), (255, 191), (300, 64))],
+    *[_case("f32", 1, 2, 2, n, m, d) for n, m, d in ((31, 33, 128), (64, 64, 64), (65, 130, 64), (129, 31, 32), (40, 70, 16), (130, 97, 128))],
+    *[_case("bf16", 2, 3, 3, 100, 77, d) for d in (16, 32)],
+    # shared key heads: 2, 3, 8 and all
+    _case("bf16", 2, 6, 3, 70, 90, 64), _case("bf16", 1, 6, 2, 50, 128, 128, causal=True), _case("bf16", 2, 8, 1, 33, 65, 64, causal=True), _case("f32", 1, 6, 2, 45, 67, 64, causal=True),
+    _case("bf16", 1, 40, 1, 1, 100, 128),
+    # causal: square, more keys than queries, more queries than keys (rows that see nothing)
+    *[_case("bf16", 1, 2, 2, n, m, d, causal=True) for n, m, d in ((1, 1, 64), (64, 64, 64), (65, 65, 128), (200, 200, 64), (33, 200, 64), (200, 33, 64), (5, 300, 128), (300, 5, 32), (513, 513, 64))],
+    *[_case("f32", 1, 2, 1, n, m, 64, causal=True) for n, m in ((70, 70), (20, 90), (90, 20))],
+    # lengths: zeros, ones, whole, beyond the tensor, below 0
+    _case("bf16", 4, 2, 2, 80, 100, 64, lens=(None, [100, 0, 1, 65])),
+    _case("bf16", 4, 2, 1, 130, 130, 128, causal=True, lens=([130, 1, 0, 77], [130, 1, 0, 77])),
+    _case("bf16", 5, 2, 1, 70, 90, 64, causal=True, lens=([70, 64, 3, 70, 500], [90, 10, 90, 0, -4])),
+    _case("f32", 3, 2, 1, 40, 60, 32, causal=True, lens=([40, 40, 7], [60, 20, 33])),
+    _case("bf16", 3, 4, 4, 100, 100, 64, lens=([100, 40, 0], None)),
+    # layouts
+    *[_case("bf16", 2, 4, 2, 75, 75, 64, causal=True, layout=s) for s in ("tokens", "piece")],
+    *[_case("f32", 2, 4, 2, 45, 45, 32, lens=(None, [45, 20]), layout=s) for s in ("tokens", "piece")],
+    # long axes with few of the other: split and joined
+    _case("bf16", 1, 2, 1, 1, 5001, 128), _case("bf16", 2, 4, 1, 3, 4100, 64, lens=(None, [4100, 129])), _case("bf16", 1, 2, 2, 4100, 3, 64), _case("bf16", 1, 1, 1, 3000, 70, 128, causal=True),
+    _case("f32", 1, 2, 1, 2, 3001, 64), _case("f32", 1, 1, 1, 3001, 2, 64), _case("bf16", 1, 8, 2, 16, 2000, 64, causal=True),
+    # middling
+    _case("bf16", 1, 4, 4, 1024, 1024, 64), _case("bf16", 1, 4, 2, 1000, 1100, 128, causal=True), _case("f32", 1, 2, 2, 512, 512, 64), _case("bf16", 1, 2, 2, 700, 700, 32), _case("bf16", 1, 2, 2, 600, 600, 16, causal=True),
+    # a sharp softmax: scores of tens
+    _case("bf16", 1, 2, 2, 150, 150, 64, sm_scale=1.0), _case("f32", 1, 2, 2, 100, 100, 64, sm_scale=1.0),
+    # the kernels of one wave a row
+    _case("bf16", 2, 4, 2, 40, 50, 64, causal=True, lens=([40, 17], [50, 9]), path=1), _case("f32", 1, 2, 1, 33, 20, 128, path=1), _case("bf16", 1, 2, 1, 20, 33, 16, causal=True, path=1),
+]
+
+
+@pytest.mark.parametrize("c", CASES, ids=_id)
+def test_dense_against_64_bits(c):
+    x = _inputs(c)
+    _check(c, _run(c, *x), *x)
+
+
+@pytest.mark.parametrize("path", [0, 1])
+@pytest.mark.parametrize("dtype,d,bad", [("bf16", 64, math.nan), ("bf16", 128, math.inf), ("f32", 32, -math.inf), ("bf16", 16, math.nan)])
+def test_nothing_behind_a_mask_is_seen(dtype, d, bad, path):
+    """Infinities and NaN behind the lengths and in keys and queries that a causal mask hides: what is not masked is as if they were zeros."""
+    c = _case(dtype, 2, 4, 2, 100, 100, d, causal=True, lens=([100, 40], [100, 40]), path=path)
+    Q, K, V, dO, ql, kl = _inputs(c)
+    clean = [t.clone() for t in (Q, K, V, dO)]
+    for t in (Q, K, V, dO):
+        t[1, :, 40:] = bad                          # behind the lengths
+    K[0, 0, 71], V[0, 0, 71, 3] = bad, bad         # seen by queries 71 and on
+    got = _run(c, Q, K, V, dO, ql, kl)
+    want = _run(c, *clean, ql, kl)
+    for n in ("O", "LSE", "dQ"):
+        assert torch.equal(got[n][1], want[n][1]) and torch.equal(got[n][0, 2:], want[n][0, 2:]), n
+        g, w = got[n][0, :2, :71].double(), want[n][0, :2, :71].double()
+        assert torch.isfinite(g).all()
+        assert float((g - w).abs().max()) <= 2.0 ** -6 * float(w.abs().max()), n      # another kernel's rounding: a few of P's and the result's half steps
+    for n in ("dK", "dV"):
+        assert torch.equal(got[n][1], want[n][1]) and torch.equal(got[n][0, 1], want[n][0, 1]), n
+    # a query and its gradient that hold a NaN: keys behind it do not see it
+    Q, K, V, dO = clean
+    Q[0, 1, 20, 1], dO[0, 1, 30, 2] = bad, bad
+    got2 = _run(c, Q, K, V, dO, ql, kl)
+    keep = [i for i in range(100) if i != 20]
+    assert torch.isfinite(got2["O"][0, 1, keep].float()).all() and torch.equal(got2["O"][0, [0, 2, 3]], want["O"][0, [0, 2, 3]])
+    for n in ("dK", "dV"):
+        g, w = got2[n][0, 0, 31:].double(), want[n][0, 0, 31:].double()
+        assert torch.isfinite(g).all() and float((g - w).abs().max()) <= 2.0 ** -6 * float(w.abs().max()), n
+
+
+def test_dense_is_the_same_bits_from_call_to_call_and_stream_to_stream():
+    c = _case("bf16", 2, 4, 2, 300, 700, 64, causal=True)
+    x = _inputs(c)
+    first = _run(c, *x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = _run(c, *x)
+    for n in first:
+        assert torch.equal(first[n], second[n]), n
+
+
+@pytest.mark.parametrize("c", [_case("bf16", 2, 4, 2, 200, 200, 64, causal=True), _case("bf16", 1, 2, 1, 1, 3000, 128), _case("f32", 1, 2, 2, 60, 60, 32)], ids=_id)
+def test_dense_replays_from_a_graph(c):
+    """A step captured into a graph, replayed with the program's own work on the same workspace between the replays; then with other inputs and
+    other lengths in the same buffers."""
+    Q, K, V, dO, _, _ = _inputs(c)
+    kl = torch.full((c["batch"],), c["Nkv"], dtype=torch.int32, device="cuda")
+    p = _plan(c, Q, K, V)
+    ws, O, LSE = p.alloc_workspace(True), p.empty("o"), torch.empty(c["batch"], c["heads"], c["Nq"], device="cuda")
+    grads = [p.empty(w) for w in "qkv"]
+
+    def step():
+        llsa.dense_forward(p, Q, K, V, None, kl, O, LSE, ws)
+        llsa.dense_backward(p, Q, K, V, O, LSE, dO, None, kl, *grads, ws)
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step()
+    for rep in range(4):
+        new = _inputs(c, seed=rep)
+        for t, n in zip((Q, K, V, dO), new):
+            t.copy_(n)
+        kl.fill_(max(1, c["Nkv"] - 37 * rep))
+        step()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in (O, LSE, *grads)]
+        ws.fill_(0xff)
+        for t in (O, LSE, *grads):
+            t.fill_(math.nan)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, w in zip((O, LSE, *grads), want):
+            assert torch.equal(t, w), rep
+
+
+def test_dense_reads_broadcast_keys_and_offsets_beyond_32_bits():
+    """Keys and values 2 MB apart, the last of them more than 4 GB behind the first, and one set of keys for all batch entries (a stride of 0)."""
+    gen = torch.Generator().manual_seed(5)
+    n, step = 2200, 1 << 20
+    store = torch.zeros(n * step, dtype=torch.bfloat16, device="cuda")
+    at = lambda off: store.as_strided((2, 1, n, 64), (0, 0, step, 1), off)
+    K, V = at(0), at(64)
+    kv = [torch.randn(1, 1, n, 64, generator=gen).to(torch.bfloat16).cuda() for _ in range(2)]
+    for t, s in ((K, kv[0]), (V, kv[1])):
+        t[0, 0].copy_(s[0, 0])
+    for Nq, causal in ((3, False), (150, True)):
+        Q = torch.randn(2, 2, Nq, 64, generator=gen).to(torch.bfloat16).cuda()
+        p = llsa.DensePlan(2, 2, Nq, n, 64, kv_heads=1, causal=causal, k_stride=(0, 0, step), v_stride=(0, 0, step))
+        O, LSE = llsa.dense_forward(p, Q, K, V)
+        want, tol = R.dense(Q, kv[0].expand(2, 1, n, 64), kv[1].expand(2, 1, n, 64), None, causal, dtype=torch.bfloat16)
+        assert bool(((O.double() - want["O"]).abs() <= tol["O"]).all()) and bool(((LSE.double() - want["LSE"]).abs() <= tol["LSE"]).all())
+    del store, K, V
+
+
+def test_dense_binding_refuses_what_does_not_fit():
+    c = _case("bf16", 2, 2, 2, 40, 40, 64)
+    Q, K, V, dO, _, _ = _inputs(c)
+    p = _plan(c, Q, K, V)
+    lens = torch.tensor([40, 40], dtype=torch.int32, device="cuda")
+    for args in ((Q.float(), K, V), (Q, K[:, :, :39], V), (Q, K.transpose(1, 2).contiguous().transpose(1, 2), V), (Q, K, V.cpu())):
+        with pytest.raises(llsa.LlsaError):
+            llsa.dense_forward(p, *args)
+    for bad in (lens.long(), lens[:1], lens.cpu()):
+        with pytest.raises(llsa.LlsaError):
+            llsa.dense_forward(p, Q, K, V, bad)
+    O, LSE = llsa.dense_forward(p, Q, K, V)
+    with pytest.raises(llsa.LlsaError):
+        llsa.dense_backward(p, Q, K, V, O, LSE, dO, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(llsa.LlsaError):
+        llsa.dense_backward(p, Q, K, V, O, LSE.half(), dO)
