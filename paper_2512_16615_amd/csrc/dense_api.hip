@@ -47,6 +47,7 @@ static llsa_status build_dense_plan(const llsa_dense_desc &d, DensePlan &p) {
     if (d.d != 16 && d.d != 32 && d.d != 64 && d.d != 128) return LLSA_ERR_UNSUPPORTED;
     if ((d.causal != 0 && d.causal != 1) || (d.kernel_path != 0 && d.kernel_path != 1)) return LLSA_ERR_UNSUPPORTED;
     p.G = d.heads / d.kv_heads;
+    if ((int64_t)d.batch * d.kv_heads * ((d.Nq * p.G + 31) / 32 + (d.Nkv + 31) / 32) >= ((int64_t)1 << 29)) return LLSA_ERR_UNSUPPORTED;   // launch grids
     // rows and keys are counted in 31 bits, groups are the grid's second dimension
     if (d.Nq > ((int64_t)1 << 30) || d.Nkv > ((int64_t)1 << 30) || d.Nq * p.G > ((int64_t)1 << 30)) return LLSA_ERR_UNSUPPORTED;
     if ((int64_t)d.batch * d.kv_heads > 65535) return LLSA_ERR_UNSUPPORTED;
@@ -61,9 +62,43 @@ static llsa_status build_dense_plan(const llsa_dense_desc &d, DensePlan &p) {
     if (!dense_apart(p.o, d.batch, d.heads, d.Nq, row)) return LLSA_ERR_BAD_SHAPE;
     p.grads = dense_apart(p.q, d.batch, d.heads, d.Nq, row) && dense_apart(p.k, d.batch, d.kv_heads, d.Nkv, row) &&
               dense_apart(p.v, d.batch, d.kv_heads, d.Nkv, row);
-    p.D_off = 0;
-    p.ws_bwd = dense_align((size_t)d.batch * d.heads * d.Nq * sizeof(float));
+    // offsets inside a tile are 32-bit
+    if (d.kernel_path == 0) {
+        const int64_t most = ((int64_t)1 << 32) - (1 << 20);
+        if (256 * p.k.token > most || 256 * p.v.token > most || (p.G - 1) * p.q.head + 256 * p.q.token > most || (p.G - 1) * p.o.head + 256 * p.o.token > most)
+            return LLSA_ERR_UNSUPPORTED;
+    }
+    p.fwd_splits = d.kernel_path ? 1 : dense_fwd_splits(p);
+    p.dq_splits = d.kernel_path ? 1 : dense_dq_splits(p);
+    p.dkv_splits = d.kernel_path ? 1 : dense_dkv_splits(p);
+    p.ws_fwd = dense_part_bytes(p, p.rows, p.fwd_splits, d.d + 2);
+    p.stat_rows = (p.rows + 127) / 128 * 128;
+    const size_t stat = dense_align((size_t)d.batch * d.kv_heads * p.stat_rows * sizeof(float));
+    p.nD_off = 0;
+    p.nlse_off = stat;
+    p.part_off = 2 * stat;
+    p.ws_bwd = p.part_off + std::max(dense_part_bytes(p, p.rows, p.dq_splits, d.d), dense_part_bytes(p, d.Nkv, p.dkv_splits, 2 * d.d));
     return LLSA_OK;
+}
+
+DenseGrid dense_grid(const DensePlan &p, int64_t rows, int tile, int splits, int row_floats, float *part) {
+    DenseGrid g;
+    memset(&g, 0, sizeof(g));
+    g.rows = rows;
+    g.groups = (uint32_t)(p.desc.batch * p.desc.kv_heads);
+    g.splits = splits;
+    const int64_t tiles = (rows + tile - 1) / tile;
+    g.by_tiles = FastDiv(tiles);
+    g.by_splits = FastDiv(splits);
+    g.by_rest = FastDiv((int64_t)g.groups * splits);
+    g.wgs = (uint32_t)(tiles * g.groups * splits);
+    g.part = part;
+    if (splits > 1) g.stat = part + (int64_t)splits * g.groups * rows * row_floats;
+    return g;
+}
+
+size_t dense_part_bytes(const DensePlan &p, int64_t rows, int splits, int row_floats) {
+    return splits == 1 ? 0 : dense_align((size_t)splits * p.desc.batch * p.desc.kv_heads * rows * row_floats * sizeof(float));
 }
 
 static DenseArgs dense_args(const DensePlan &p, const void *Q, const void *K, const void *V, const int32_t *q_lens, const int32_t *kv_lens, float *LSE) {
@@ -82,6 +117,7 @@ static DenseArgs dense_args(const DensePlan &p, const void *Q, const void *K, co
     a.G = p.G;
     a.div_g = FastDiv(p.G);
     a.causal = p.desc.causal;
+    a.stat_rows = p.stat_rows;
     a.scale = p.scale;
     a.scale2 = p.scale * 1.4426950408889634f;
     return a;
@@ -123,7 +159,9 @@ llsa_status llsa_dense_forward(const llsa_dense_plan_t *plan, const void *Q, con
     if (any_off_grid(16, Q, K, V, O, LSE) || any_off_grid(4, q_lens, kv_lens) || off_grid(workspace, 256)) return LLSA_ERR_BAD_SHAPE;
     DenseArgs a = dense_args(plan->p, Q, K, V, q_lens, kv_lens, LSE);
     a.out = static_cast<char *>(O);
-    return launch_dense_fwd_rows(plan->p, a, (hipStream_t)hip_stream) == hipSuccess ? LLSA_OK : LLSA_ERR_RUNTIME;
+    hipStream_t s = (hipStream_t)hip_stream;
+    const hipError_t e = plan->p.desc.kernel_path ? launch_dense_fwd_rows(plan->p, a, s) : launch_dense_fwd(plan->p, a, static_cast<float *>(workspace), s);
+    return e == hipSuccess ? LLSA_OK : LLSA_ERR_RUNTIME;
 }
 
 llsa_status llsa_dense_backward(const llsa_dense_plan_t *plan, const void *Q, const void *K, const void *V, const int32_t *q_lens,
@@ -138,10 +176,15 @@ llsa_status llsa_dense_backward(const llsa_dense_plan_t *plan, const void *Q, co
     a.dQ = static_cast<char *>(dQ);
     a.dK = static_cast<char *>(dK);
     a.dV = static_cast<char *>(dV);
-    a.D = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->p.D_off);
+    a.nD = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->p.nD_off);
+    a.nlse = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->p.nlse_off);
     hipStream_t s = (hipStream_t)hip_stream;
-    if (launch_dense_dq_rows(plan->p, a, s) != hipSuccess || launch_dense_dkv_rows(plan->p, a, s) != hipSuccess) return LLSA_ERR_RUNTIME;
-    return LLSA_OK;
+    if (plan->p.desc.kernel_path) {
+        if (launch_dense_dq_rows(plan->p, a, s) != hipSuccess || launch_dense_dkv_rows(plan->p, a, s) != hipSuccess) return LLSA_ERR_RUNTIME;
+        return LLSA_OK;
+    }
+    float *part = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->p.part_off);
+    return launch_dense_bwd(plan->p, a, part, s) == hipSuccess ? LLSA_OK : LLSA_ERR_RUNTIME;
 }
 
 }  // extern "C"

@@ -1,0 +1,219 @@
+// Dense attention, forward: workgroups of 4 waves, 32 QB rows each (a row: a query of one of the heads that share a key head), keys and values in
+// tiles of KT through LDS, the running maximum and sum of a softmax in registers.  A lane has one row: its scores come out of the first product in the
+// registers that the second one takes, O^T = V^T P^T collects channels in the registers of the same lane, so maximum, sum and rescaling are
+// the lane's own (and its partner's in the other half of the wave).
+#include "dense_row.h"
+#include "dense_tile.h"
+
+#include <type_traits>
+
+namespace llsa {
+
+// waves a SIMD that the registers are shared out for
+template <class T, int D, int QB> constexpr int fwd_waves() { return D * (int)sizeof(T) * QB <= 256 ? 2 : 1; }
+
+template <class T, int D, int QB, int KT>
+__global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
+    using Tile = DenseTile<T, D>;
+    using Loads = TileLoads<T, D, KT, 4>;
+    constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32;
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][TILEB];      // stage; keys, values
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
+    const DenseWork work = dense_work(grid, a.causal, true);
+    const DenseGroup p(a, work.group);
+    const Tile tile(lane);
+    const int64_t row0 = (int64_t)work.tile * (128 * QB), wrow0 = row0 + wave * (32 * QB);
+    const int end = key_span(a, p, row0, row0 + 128 * QB - 1).some;
+    const KeySpan mine = key_span(a, p, wrow0, wrow0 + 32 * QB - 1);
+
+    // the wave's rows as operands, and what each sees
+    Piece<T> q[QB][Tile::KS];
+    int seen[QB], qi[QB], qg[QB];
+#pragma unroll
+    for (int c = 0; c < QB; ++c) {
+        const int64_t r = wrow0 + 32 * c + col;
+        const bool in = r < grid.rows;
+        qi[c] = (int)a.div_g((uint32_t)(in ? r : 0));
+        qg[c] = (int)((in ? r : 0) - (int64_t)qi[c] * a.G);
+        seen[c] = in ? p.seen(a, qi[c]) : 0;
+        if (!in) qi[c] = -1;
+        const char *src = p.Q + qg[c] * a.q.head + (int64_t)max(qi[c], 0) * a.q.token + 16 * h;
+#pragma unroll
+        for (int ks = 0; ks < Tile::KS; ++ks) q[c][ks].w = seen[c] > 0 ? *reinterpret_cast<const u32x4 *>(src + 32 * ks) : u32x4{0, 0, 0, 0};
+    }
+
+    f32x16 o[QB][Tile::NB];
+    float m[QB], l[QB];                                      // the reference that the exponentials are relative to (log2), their sum in this lane
+#pragma unroll
+    for (int c = 0; c < QB; ++c) {
+#pragma unroll
+        for (int n = 0; n < Tile::NB; ++n)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[c][n][e] = 0.f;
+        m[c] = -3e38f;
+        l[c] = 0.f;
+    }
+
+    const int tiles = (end + KT - 1) / KT, per = (tiles + grid.splits - 1) / grid.splits;
+    const int t0 = work.split * per, t1 = min(tiles, t0 + per);
+    auto fetch = [&](int t) {
+        const int k0 = t * KT, left = min(KT, p.nk - k0);
+        const unsigned lds0 = lds_address(&lds[t & 1][0][0]);
+        const unsigned kt = (unsigned)a.k.token, vt = (unsigned)a.v.token;
+        Loads::keys(buffer_of(p.K + k0 * a.k.token, (left - 1) * kt + Tile::ROWB), kt, lds0, wave, lane);
+        Loads::keys(buffer_of(p.V + k0 * a.v.token, (left - 1) * vt + Tile::ROWB), vt, lds0 + TILEB, wave, lane);
+    };
+    if (t0 < t1) fetch(t0);
+    for (int t = t0; t < t1; ++t) {
+        vm_wait_barrier<0>();                                // tile t is there, and nobody reads the other stage
+        if (t + 1 < t1) fetch(t + 1);
+        const int k0 = t * KT;
+        if (k0 >= mine.some) continue;
+        const char *kt = &lds[t & 1][0][0], *vt = &lds[t & 1][1][0];
+        f32x16 s[SUBS][QB];
+#pragma unroll
+        for (int u = 0; u < SUBS; ++u) {
+#pragma unroll
+            for (int c = 0; c < QB; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[u][c][e] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < Tile::KS; ++ks) {
+                const Piece<T> k = tile.row(kt, u, ks);
+#pragma unroll
+                for (int c = 0; c < QB; ++c) s[u][c] = piece_product(k, q[c][ks], s[u][c]);
+            }
+        }
+        if (k0 + KT > mine.all) {                            // a key that some row does not see
+#pragma unroll
+            for (int c = 0; c < QB; ++c) {
+                const int lim = seen[c] - k0 - 4 * h;
+#pragma unroll
+                for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[u][c][e] = 32 * u + 8 * (e >> 2) + (e & 3) < lim ? s[u][c][e] : -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < QB; ++c) {
+            float mx = s[0][c][0];
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][c][e]);
+            mx = half_max(mx) * a.scale2;
+            // The reference follows the maximum only once that is 2^8 beyond it (the sums stay far from fp32's range), for all rows of the wave
+            // at once: after the first tiles the accumulators are hardly ever rescaled.
+            if (__builtin_amdgcn_ballot_w64(mx > m[c] + 8.f)) {
+                const float m2 = fmaxf(m[c], mx), f = __builtin_amdgcn_exp2f(m[c] - m2);
+                m[c] = m2;
+                l[c] *= f;
+#pragma unroll
+                for (int n = 0; n < Tile::NB; ++n)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[c][n][e] *= f;
+            }
+            Probs<T> pr[SUBS];
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    s[u][c][e] = __builtin_amdgcn_exp2f(fmaf(s[u][c][e], a.scale2, -m[c]));
+                    l[c] += s[u][c][e];
+                }
+                pr[u].set(s[u][c]);
+            }
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int n = 0; n < Tile::NB; ++n) o[c][n] = tile.col_product(vt, u, n, pr[u], o[c][n]);
+        }
+    }
+
+#pragma unroll
+    for (int c = 0; c < QB; ++c) {
+        const float sum = half_sum(l[c]);
+        if (grid.splits > 1) {
+            const int64_t at = ((int64_t)work.split * grid.groups + work.group) * grid.rows + wrow0 + 32 * c + col;
+            if (qi[c] >= 0) {
+                store_partial<D>(grid.part + at * D, o[c], h);
+                if (h == 0) *reinterpret_cast<float2 *>(grid.stat + 2 * at) = make_float2(m[c], sum);
+            }
+            continue;
+        }
+        const bool any = seen[c] > 0;
+        const float f = any ? 1.f / sum : 0.f;
+        keep_rows(o[c], any);
+        uint64_t redo = 0;
+        if (a.causal) {                                      // a key that some row of the tile does not see may have met it as 0 times an infinity
+#pragma unroll
+            for (int n = 0; n < Tile::NB; ++n)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[c][n][e] *= f;
+            redo = not_finite(o[c]) & __builtin_amdgcn_ballot_w64(any);
+            redo = (redo | redo >> 32) & 0xffffffffu;
+        }
+        char *dst = p.out + qg[c] * a.o.head + (int64_t)max(qi[c], 0) * a.o.token;
+        store_rows<T, D>(dst, o[c], a.causal ? 1.f : f, h, qi[c] >= 0);
+        if (h == 0 && qi[c] >= 0) p.LSE[(int64_t)qg[c] * a.Nq + qi[c]] = any ? (m[c] + __log2f(sum)) * kLn2 : -INFINITY;
+        while (redo) {
+            const int i = __builtin_ctzll(redo);
+            redo &= redo - 1;
+            dense_row_forward<T, D>(a, p, __builtin_amdgcn_readlane(qi[c], i), __builtin_amdgcn_readlane(qg[c], i), lane);
+        }
+    }
+}
+
+// The splits' partial sums of a row, one wave a row: the exponentials of split i are relative to its own reference.
+template <class T, int D> __global__ void __launch_bounds__(256) dense_join_kernel(DenseArgs a, DenseGrid grid) {
+    using Row = LaneRow<T, D>;
+    const int lane = threadIdx.x & 63;
+    const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= grid.rows) return;
+    const DenseGroup p(a, blockIdx.y);
+    const int i = (int)a.div_g((uint32_t)r), g = (int)(r - (int64_t)i * a.G);
+    char *dst = p.out + g * a.o.head + i * a.o.token;
+    const bool any = p.seen(a, i) > 0;
+    float m = -3e38f, l = 0.f;
+    for (int s = 0; s < grid.splits; ++s) m = fmaxf(m, grid.stat[2 * (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r)]);
+    Row acc = Row::zero();
+    for (int s = 0; s < grid.splits; ++s) {
+        const int64_t at = ((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r;
+        const float2 st = *reinterpret_cast<const float2 *>(grid.stat + 2 * at);
+        const float f = __builtin_amdgcn_exp2f(st.x - m);
+        l = fmaf(f, st.y, l);
+        acc.add_part(grid.part + at * D, f, lane);
+    }
+    if (any) acc.scale(1.f / l);
+    else acc = Row::zero();
+    if (a.causal && any && !acc.finite()) {
+        dense_row_forward<T, D>(a, p, i, g, lane);
+        return;
+    }
+    acc.store(dst, lane);
+    if (lane == 0) p.LSE[(int64_t)g * a.Nq + i] = any ? (m + __log2f(l)) * kLn2 : -INFINITY;
+}
+
+// Two workgroups a CU's worth of tiles need no splitting; fewer rows share out the keys, at least 4 tiles of 64 each.
+int dense_fwd_splits(const DensePlan &p) {
+    const int64_t base = (int64_t)p.desc.batch * p.desc.kv_heads * ((p.rows + 127) / 128), tiles = (p.desc.Nkv + 63) / 64;
+    if (base >= 256) return 1;
+    const int64_t want = (512 + base - 1) / base, most = tiles / 4;
+    return (int)(most < 2 ? 1 : want < most ? want : most);
+}
+
+template <class T, int D> static hipError_t launch_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
+    constexpr int KT = DenseTile<T, D>::ROWB > 256 ? 32 : 64;
+    DenseGrid g = dense_grid(p, p.rows, 128, p.fwd_splits, D, ws);
+    dense_fwd_kernel<T, D, 1, KT><<<g.wgs, 256, 0, s>>>(a, g);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || g.splits == 1) return e;
+    dense_join_kernel<T, D><<<dim3((unsigned)((p.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);
+    return hipGetLastError();
+}
+
+hipError_t launch_dense_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
+    return dense_dispatch(p, [&](auto t, auto d) { return launch_fwd<decltype(t), decltype(d)::value>(p, a, ws, s); });
+}
+
+}  // namespace llsa

@@ -47,6 +47,19 @@ template <class T, int D> struct LaneRow {
 #pragma unroll
         for (int k = 0; k < n; ++k) x[k] = fmaf(f, o.x[k], x[k]);
     }
+    // += f times d partial sums
+    __device__ __forceinline__ void add_part(const float *part, float f, int lane) {
+#pragma unroll
+        for (int k = 0; k < n; ++k)
+            if (lane + 64 * k < D) x[k] = fmaf(f, part[lane + 64 * k], x[k]);
+    }
+    // in every lane of the wave
+    __device__ __forceinline__ bool finite() const {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < n; ++k) s = fmaf(x[k], 0.f, s);
+        return __builtin_amdgcn_ballot_w64(s != 0.f) == 0;
+    }
     __device__ __forceinline__ float dot(const LaneRow &o) const {
         float s = 0.f;
 #pragma unroll
@@ -86,6 +99,29 @@ struct DenseGroup {
     __device__ __forceinline__ int first_query(const DenseArgs &a, int j) const { return j >= nk ? nq : a.causal ? min(nq, max(0, j - nk + nq)) : 0; }
 };
 
+// Keys of a row seen by the rows first .. last of a group
+struct KeySpan { int all, some; };                          // keys that every one of them sees; that one of them sees
+__device__ __forceinline__ KeySpan key_span(const DenseArgs &a, const DenseGroup &p, int64_t first, int64_t last) {
+    const int i0 = (int)min(first, (int64_t)0x7fffffff), i1 = (int)min(last, (int64_t)0x7fffffff);
+    const int q0 = (int)a.div_g(i0), q1 = min((int)a.div_g(i1), p.nq - 1);
+    if (q0 >= p.nq) return {0, 0};
+    return {p.seen(a, q0), p.seen(a, q1)};
+}
+
+// Which rows and keys a workgroup has.  Causal: the tiles with the most work first (the last
+// rows, the first keys), of all groups in turn; otherwise the tiles of a group next to each
+// other and the groups in stretches, so that the workgroups of one XCD share their keys.
+struct DenseWork { int group, split, tile; };
+__device__ __forceinline__ DenseWork dense_work(const DenseGrid &g, int causal, bool last_first) {
+    if (causal) {
+        const unsigned t = g.by_rest(blockIdx.x), rest = blockIdx.x - t * g.by_rest.d;
+        const unsigned group = g.by_splits(rest);
+        return {(int)group, (int)(rest - group * g.by_splits.d), (int)(last_first ? g.by_tiles.d - 1 - t : t)};
+    }
+    const unsigned w = xcd_contiguous32(blockIdx.x, gridDim.x), rest = g.by_tiles(w), group = g.by_splits(rest);
+    return {(int)group, (int)(rest - group * g.by_splits.d), (int)(w - rest * g.by_tiles.d)};
+}
+
 template <class T, int D> __device__ __forceinline__ void dense_row_forward(const DenseArgs &a, const DenseGroup &p, int i, int g, int lane) {
     using Row = LaneRow<T, D>;
     const Row q = Row::load(p.Q + g * a.q.head + i * a.q.token, lane);
@@ -110,8 +146,8 @@ template <class T, int D> __device__ __forceinline__ void dense_row_forward(cons
     if (lane == 0) p.LSE[(int64_t)g * a.Nq + i] = n > 0 ? m + __logf(l) : -INFINITY;
 }
 
-// D of the row comes as an argument: both passes of the backward use the same one
-template <class T, int D> __device__ __forceinline__ void dense_row_dq(const DenseArgs &a, const DenseGroup &p, int i, int g, float delta, int lane) {
+// nD: minus D of the row
+template <class T, int D> __device__ __forceinline__ void dense_row_dq(const DenseArgs &a, const DenseGroup &p, int i, int g, float nD, int lane) {
     using Row = LaneRow<T, D>;
     Row acc = Row::zero();
     const int n = p.seen(a, i);
@@ -121,15 +157,15 @@ template <class T, int D> __device__ __forceinline__ void dense_row_dq(const Den
         for (int j = 0; j < n; ++j) {
             const Row k = Row::load(p.K + j * a.k.token, lane);
             const float e = __expf(q.dot(k) * a.scale - lse);
-            acc.add(e * (go.dot(Row::load(p.V + j * a.v.token, lane)) - delta), k);
+            acc.add(e * (go.dot(Row::load(p.V + j * a.v.token, lane)) + nD), k);
         }
         acc.scale(a.scale);
     }
     acc.store(p.dQ + g * a.q.head + i * a.q.token, lane);
 }
 
-// delta: D of the group's rows (row i * G + g)
-template <class T, int D> __device__ __forceinline__ void dense_row_dkv(const DenseArgs &a, const DenseGroup &p, int j, const float *delta, int lane) {
+// nD: minus D of the group's rows (row i * G + g)
+template <class T, int D> __device__ __forceinline__ void dense_row_dkv(const DenseArgs &a, const DenseGroup &p, int j, const float *nD, int lane) {
     using Row = LaneRow<T, D>;
     Row dk = Row::zero(), dv = Row::zero();
     const int first = p.first_query(a, j);
@@ -140,7 +176,7 @@ template <class T, int D> __device__ __forceinline__ void dense_row_dkv(const De
                 const Row q = Row::load(p.Q + g * a.q.head + i * a.q.token, lane), go = Row::load(p.dO + g * a.o.head + i * a.o.token, lane);
                 const float e = __expf(q.dot(k) * a.scale - p.LSE[(int64_t)g * a.Nq + i]);
                 dv.add(e, go);
-                dk.add(e * (go.dot(v) - delta[(int64_t)i * a.G + g]), q);
+                dk.add(e * (go.dot(v) + nD[(int64_t)i * a.G + g]), q);
             }
         dk.scale(a.scale);
     }

@@ -23,8 +23,8 @@ template <class T, int D> __global__ void __launch_bounds__(256) dense_dq_rows_k
     const int64_t at = g * a.o.head + i * a.o.token;
     float delta = 0.f;
     if (p.seen(a, i) > 0) delta = Row::load(p.dO + at, lane).dot(Row::load(p.O + at, lane));
-    if (lane == 0) a.D[blockIdx.y * rows + r] = delta;
-    dense_row_dq<T, D>(a, p, i, g, delta, lane);
+    if (lane == 0) a.nD[blockIdx.y * a.stat_rows + r] = -delta;
+    dense_row_dq<T, D>(a, p, i, g, -delta, lane);
 }
 
 template <class T, int D> __global__ void __launch_bounds__(256) dense_dkv_rows_kernel(DenseArgs a, int64_t rows) {
@@ -32,27 +32,15 @@ template <class T, int D> __global__ void __launch_bounds__(256) dense_dkv_rows_
     const int64_t j = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (j >= a.Nkv) return;
     const DenseGroup p(a, blockIdx.y);
-    dense_row_dkv<T, D>(a, p, (int)j, a.D + blockIdx.y * rows, lane);
+    dense_row_dkv<T, D>(a, p, (int)j, a.nD + blockIdx.y * a.stat_rows, lane);
 }
 
 #define LLSA_DENSE_ROWS(kernel, count)                                                                             \
     const dim3 grid((unsigned)(((count) + 3) / 4), (unsigned)(p.desc.batch * p.desc.kv_heads));                     \
-    auto go = [&](auto t, auto d) { kernel<decltype(t), decltype(d)::value><<<grid, 256, 0, s>>>(a, p.rows); };     \
-    dense_dispatch(p, go);                                                                                          \
-    return hipGetLastError();
-
-template <class F> static void dense_dispatch(const DensePlan &p, F go) {
-    auto by_d = [&](auto t) {
-        switch (p.desc.d) {
-            case 16: go(t, std::integral_constant<int, 16>()); break;
-            case 32: go(t, std::integral_constant<int, 32>()); break;
-            case 64: go(t, std::integral_constant<int, 64>()); break;
-            default: go(t, std::integral_constant<int, 128>()); break;
-        }
-    };
-    if (p.elt == 4) by_d(float());
-    else by_d(__bf16());
-}
+    return dense_dispatch(p, [&](auto t, auto d) {                                                                  \
+        kernel<decltype(t), decltype(d)::value><<<grid, 256, 0, s>>>(a, p.rows);                                    \
+        return hipGetLastError();                                                                                   \
+    });
 
 hipError_t launch_dense_fwd_rows(const DensePlan &p, const DenseArgs &a, hipStream_t s) { LLSA_DENSE_ROWS(dense_fwd_rows_kernel, p.rows) }
 hipError_t launch_dense_dq_rows(const DensePlan &p, const DenseArgs &a, hipStream_t s) { LLSA_DENSE_ROWS(dense_dq_rows_kernel, p.rows) }
