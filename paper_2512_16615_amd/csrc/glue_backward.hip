@@ -121,19 +121,22 @@ template <class T, int D> __global__ void __launch_bounds__(256) glue_bwd_kernel
     }
 }
 
-// one workgroup: a wave's worth of slices of every column, then the slices in order
+// The workgroups' sums added up: 64 slices of 16 columns a workgroup, each slice every 64th workgroup's, then the slices in order.
 template <int D> __global__ void __launch_bounds__(1024) glue_sums_kernel(GlueBwdArgs a) {
-    constexpr int SL = 1024 / (2 * D);
-    __shared__ float lds[SL][2 * D];
-    const int c = threadIdx.x % (2 * D), sl = threadIdx.x / (2 * D);
+    __shared__ float lds[64][17];
+    const int col = threadIdx.x & 15, c = blockIdx.x * 16 + col, slice = threadIdx.x >> 4;
     float s = 0.f;
-    for (int w = sl; w < a.wgs; w += SL) s += a.part[(int64_t)w * 2 * D + c];
-    lds[sl][c] = s;
+#pragma unroll 8
+    for (int w = slice; w < a.wgs; w += 64) s += a.part[(int64_t)w * 2 * D + c];
+    lds[slice][col] = s;
     __syncthreads();
-    if (sl == 0) {
+    if (slice < 4) {                                         // 16 slices each, then those four
         s = 0.f;
-        for (int i = 0; i < SL; ++i) s += lds[i][c];
-        a.dgamma[c / D][c % D] = s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += lds[slice * 16 + i][col];
+        s += __shfl_xor(s, 16, 64);
+        s += __shfl_xor(s, 32, 64);
+        if (slice == 0) a.dgamma[c / D][c % D] = s;
     }
 }
 
@@ -175,7 +178,7 @@ hipError_t launch_glue_backward(const Plan &p, const void *Qpre, const void *Kpr
         else            glue_bwd_kernel<__bf16, D><<<dim3(gx, gy), 256, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        glue_sums_kernel<D><<<1, 1024, 0, s>>>(a);
+        glue_sums_kernel<D><<<2 * D / 16, 1024, 0, s>>>(a);
         return hipGetLastError();
     };
     switch (p.d) {

@@ -4,10 +4,13 @@
 
 namespace llsa {
 
+struct NormShape {
+    int tpr, nv;                    // threads a row, 16-byte vectors a thread
+    int blocks;                     // workgroups a batch entry
+};
 struct NormPlan {
     llsa_norm_desc desc;
-    int tpr, nv;                    // threads a row, 16-byte vectors a thread
-    int fwd_blocks, bwd_blocks;     // workgroups a batch entry
+    NormShape fwd, bwd;
     size_t ws;
 };
 

@@ -1,5 +1,5 @@
-// The norms between two blocks with gate and residual, forward and backward: one pass over the rows, each held in registers by 16, 64, 256 or
-// 512 threads of a workgroup (at most 16 channels a thread), so that a row is read once and written once.  What varies by channel only (the gains, and the
+// The norms between two blocks with gate and residual, forward and backward: one pass over the rows, each held in registers by 16 to 1024
+// threads (at most 16 channels a thread forward, 8 backward), so that a row is read once and written once.  What varies by channel only (the gains, and the
 // modulation of the batch entry that a workgroup belongs to) stays in registers over all rows of the workgroup, combined:
 //   y = n(x') ga + sh, x' = x + gz n(branch)       with ga = gain (1 + scale), sh = shift, gz = alpha gate gain_branch.
 // Backward, per row, with h^ = n(x'), u = n(branch) (or the branch itself):
@@ -36,69 +36,146 @@ template <class T> __device__ __forceinline__ void n_unpack(const typename NVec<
         }
     }
 }
-// channels c .. c + n - 1 of a row of C, zeros beyond it
-template <class T> __device__ __forceinline__ void n_load(const T *row, int c, int C, float *x) {
-    constexpr int n = NVec<T>::n;
-    if (c + n <= C) {
-        n_unpack<T>(*reinterpret_cast<const typename NVec<T>::Raw *>(row + c), x);
-    } else {
+// Which channels of a row a thread has: NV vectors of n, number k at channel (k TPR + t) n.  FULL: the vectors cover the row exactly.  Otherwise
+// the last one that is not whole is read n channels from the row's end (so that no load needs a branch) and only its last ones are the
+// thread's own; one beyond the row has none.  What is not its own counts as zeros and is not written.
+template <class T, int TPR, int NV, bool FULL> struct Channels {
+    static constexpr int n = NVec<T>::n, E = NV * n;
+    int first[NV], own[NV], C;                               // where a vector is read, its first element that is the thread's own
+    __device__ __forceinline__ Channels(int t, int C_) : C(C_) {
 #pragma unroll
-        for (int e = 0; e < n; ++e) x[e] = c + e < C ? n_get(row + c + e) : 0.f;
-    }
-}
-template <class T> __device__ __forceinline__ void n_store(T *row, int c, int C, const float *x) {
-    constexpr int n = NVec<T>::n;
-    typename NVec<T>::Raw r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(T) == 4) {
-            r.w[i] = __float_as_uint(x[i]);
-        } else {
-            union { __bf16 h[2]; uint32_t u; } w;
-            w.h[0] = (__bf16)x[2 * i];
-            w.h[1] = (__bf16)x[2 * i + 1];
-            r.w[i] = w.u;
+        for (int k = 0; k < NV; ++k) {
+            const int c = (k * TPR + t) * n;
+            first[k] = FULL || c + n <= C ? c : c < C ? max(0, C - n) : 0;
+            own[k] = FULL || c + n <= C ? 0 : c < C ? c - first[k] : n;
         }
     }
-    if (c + n <= C) {
-        *reinterpret_cast<typename NVec<T>::Raw *>(row + c) = r;
-    } else {
+    __device__ __forceinline__ int channel(int i) const { return first[i / n] + i % n; }
+    __device__ __forceinline__ bool mine(int i) const { return FULL || (i % n >= own[i / n] && channel(i) < C); }
+    // a row's channels as they stand in memory (an element's 16 bits or 32 a register where the row has no whole vector), and as numbers
+    struct Raw { typename NVec<T>::Raw r[NV]; };
+    __device__ __forceinline__ void ask(const char *base, int64_t at, Raw &x) const {
+        const T *row = reinterpret_cast<const T *>(base) + at;
+        if (FULL || C >= n) {
 #pragma unroll
-        for (int e = 0; e < n; ++e)
-            if (c + e < C) row[c + e] = (T)x[e];
+            for (int k = 0; k < NV; ++k) x.r[k] = *reinterpret_cast<const typename NVec<T>::Raw *>(row + first[k]);
+        } else {
+            union { T v[E]; Raw r; } u;
+#pragma unroll
+            for (int i = 0; i < E; ++i) u.v[i] = mine(i) ? row[channel(i)] : (T)0.f;
+            x = u.r;
+        }
     }
-}
+    __device__ __forceinline__ void get(const Raw &r, float (&x)[E]) const {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) n_unpack<T>(r.r[k], x + k * n);
+#pragma unroll
+        for (int i = 0; !FULL && i < E; ++i) x[i] = mine(i) ? x[i] : 0.f;
+    }
+    __device__ __forceinline__ void load(const char *base, int64_t at, float (&x)[E]) const {
+        Raw r;
+        ask(base, at, r);
+        get(r, x);
+    }
+    __device__ __forceinline__ void store(char *base, int64_t at, const float (&x)[E]) const {
+        T *row = reinterpret_cast<T *>(base) + at;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (FULL || (own[k] == 0 && C >= n)) {
+                typename NVec<T>::Raw r;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (sizeof(T) == 4) {
+                        r.w[i] = __float_as_uint(x[k * n + i]);
+                    } else {
+                        union { __bf16 h[2]; uint32_t u; } w;
+                        w.h[0] = (__bf16)x[k * n + 2 * i];
+                        w.h[1] = (__bf16)x[k * n + 2 * i + 1];
+                        r.w[i] = w.u;
+                    }
+                }
+                *reinterpret_cast<typename NVec<T>::Raw *>(row + first[k]) = r;
+            } else {
+#pragma unroll
+                for (int e = 0; e < n; ++e)
+                    if (mine(k * n + e)) row[first[k] + e] = (T)x[k * n + e];
+            }
+        }
+    }
+};
 // a modulation vector's channel, of either type; `none` where it was not given
 __device__ __forceinline__ float n_mod(const char *m, int f32, int64_t at, float none) {
     return !m ? none : f32 ? reinterpret_cast<const float *>(m)[at] : n_get(reinterpret_cast<const __bf16 *>(m) + at);
 }
+// a thread's channels of a gain or a modulation vector (which may begin at any element)
+template <class Ch> __device__ __forceinline__ void channels_of(const Ch &ch, const char *m, int f32, int64_t at, float none, float (&x)[Ch::E]) {
+    constexpr int n = Ch::n;
+    if (!m) {
+#pragma unroll
+        for (int i = 0; i < Ch::E; ++i) x[i] = none;
+    } else if (ch.C < n) {
+#pragma unroll
+        for (int i = 0; i < Ch::E; ++i) x[i] = ch.mine(i) ? n_mod(m, f32, at + ch.channel(i), none) : none;
+    } else if (f32) {
+        struct __attribute__((packed, aligned(4))) Raw { float v[n]; };
+#pragma unroll
+        for (int k = 0; k < Ch::E / n; ++k) {
+            const Raw r = *reinterpret_cast<const Raw *>(reinterpret_cast<const float *>(m) + at + ch.first[k]);
+#pragma unroll
+            for (int e = 0; e < n; ++e) x[k * n + e] = r.v[e];
+        }
+    } else {
+        struct __attribute__((packed, aligned(2))) Raw { __bf16 v[n]; };
+#pragma unroll
+        for (int k = 0; k < Ch::E / n; ++k) {
+            const Raw r = *reinterpret_cast<const Raw *>(reinterpret_cast<const __bf16 *>(m) + at + ch.first[k]);
+#pragma unroll
+            for (int e = 0; e < n; ++e) x[k * n + e] = (float)r.v[e];
+        }
+    }
+}
+// what the rows of batch entry b are multiplied by (0 for the channels that are not the thread's own): alpha gate gain_branch, gain (1 + scale)
+template <class Ch> __device__ __forceinline__ void channel_factors(const NormArgs &a, const Ch &ch, int64_t at, float (&gz)[Ch::E], float (&ga)[Ch::E]) {
+    float v[Ch::E], w[Ch::E];
+    channels_of(ch, a.gate, a.mod_f32, at, 1.f, v);
+    channels_of(ch, reinterpret_cast<const char *>(a.gain_branch), 1, 0, 1.f, w);
+#pragma unroll
+    for (int i = 0; i < Ch::E; ++i) gz[i] = ch.mine(i) ? a.alpha * v[i] * w[i] : 0.f;
+    channels_of(ch, a.scale, a.mod_f32, at, 0.f, v);
+    channels_of(ch, reinterpret_cast<const char *>(a.gain), 1, 0, 1.f, w);
+#pragma unroll
+    for (int i = 0; i < Ch::E; ++i) ga[i] = ch.mine(i) ? w[i] * (1.f + v[i]) : 0.f;
+}
 
-// Sums over the TPR threads of a row, K at once, the result in each of them.  lds: K floats a wave, not read or written by another call until
-// a barrier (callers take turns with two of them).
+// threads of a workgroup: four waves with rows of their own, or one row
+constexpr int norm_threads(int tpr) { return tpr <= 64 ? 256 : tpr; }
+
+// Sums over the TPR threads of a row, K at once, the result in each of them.  lds: K floats a wave of the workgroup, not read or written by another call
+// until a barrier.  The whole workgroup calls.
 template <int TPR, int K> __device__ __forceinline__ void row_sums(float (&v)[K], float *lds) {
 #pragma unroll
     for (int o = (TPR < 64 ? TPR : 64) / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o, 64);
     if constexpr (TPR > 64) {
-        constexpr int W = TPR / 64;
-        const int w = threadIdx.x >> 6;
+        constexpr int W = TPR / 64, ALL = norm_threads(TPR) / 64;
+        const int w = threadIdx.x >> 6, w0 = w / W * W;
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int k = 0; k < K; ++k) lds[k * W + w] = v[k];
+            for (int k = 0; k < K; ++k) lds[k * ALL + w] = v[k];
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             v[k] = 0.f;
 #pragma unroll
-            for (int i = 0; i < W; ++i) v[k] += lds[k * W + i];
+            for (int i = 0; i < W; ++i) v[k] += lds[k * ALL + w0 + i];
         }
     }
 }
 
 // mean and 1 / deviation of a row held as x (zeros beyond C)
-template <int TPR, int E, bool LAYER>
-__device__ __forceinline__ void row_stats(const float (&x)[E], const bool (&in)[E], float inv_c, float eps, float *lds, float &m, float &r) {
+template <int TPR, int E, bool LAYER, class Ch>
+__device__ __forceinline__ void row_stats(const float (&x)[E], const Ch &ch, float inv_c, float eps, float *lds, float &m, float &r) {
     float s[1] = {0.f};
     m = 0.f;
     if constexpr (LAYER) {
@@ -110,109 +187,103 @@ __device__ __forceinline__ void row_stats(const float (&x)[E], const bool (&in)[
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float d = in[e] ? x[e] - m : 0.f;
+        const float d = !LAYER || ch.mine(e) ? x[e] - m : 0.f;
         s[0] = fmaf(d, d, s[0]);
     }
     row_sums<TPR, 1>(s, lds + 32);
     r = 1.f / sqrtf(fmaf(s[0], inv_c, eps));
 }
 
-template <class T, int TPR, int NV, bool LAYER>
-__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_fwd_kernel(NormArgs a) {
-    constexpr int VN = NVec<T>::n, E = NV * VN, GP = TPR > 256 ? 1 : 256 / TPR;
+template <class T, int TPR, int NV, bool LAYER, bool FULL>
+__global__ void __launch_bounds__(norm_threads(TPR)) norm_fwd_kernel(NormArgs a) {
+    using Ch = Channels<T, TPR, NV, FULL>;
+    constexpr int E = Ch::E, GP = norm_threads(TPR) / TPR;
     __shared__ float lds[4][32];
     const int t = threadIdx.x % TPR, b = blockIdx.y;
-    int ch[NV];
-    bool in[E];
+    const Ch ch(t, a.C);
     float gz[E], ga[E], sh[E];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        ch[k] = (k * TPR + t) * VN;
-#pragma unroll
-        for (int e = 0; e < VN; ++e) {
-            const int c = ch[k] + e, i = k * VN + e;
-            in[i] = c < a.C;
-            const int64_t at = b * a.mod_stride + c;
-            gz[i] = in[i] && a.branch ? a.alpha * n_mod(a.gate, a.mod_f32, at, 1.f) * (a.gain_branch ? a.gain_branch[c] : 1.f) : 0.f;
-            ga[i] = in[i] && a.y ? (a.gain ? a.gain[c] : 1.f) * (1.f + n_mod(a.scale, a.mod_f32, at, 0.f)) : 0.f;
-            sh[i] = in[i] && a.y ? n_mod(a.shift, a.mod_f32, at, 0.f) : 0.f;
-        }
-    }
+    channel_factors(a, ch, b * a.mod_stride, gz, ga);
+    channels_of(ch, a.shift, a.mod_f32, b * a.mod_stride, 0.f, sh);
     for (int64_t n = (int64_t)blockIdx.x * GP + threadIdx.x / TPR; n < a.N; n += (int64_t)gridDim.x * GP) {
         const int64_t row = b * a.N + n;
         float x[E], st[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < NV; ++k) n_load(reinterpret_cast<const T *>(a.x) + row * a.C, ch[k], a.C, x + k * VN);
+        ch.load(a.x, row * a.C, x);
         if (a.branch) {
             float u[E];
-#pragma unroll
-            for (int k = 0; k < NV; ++k) n_load(reinterpret_cast<const T *>(a.branch) + row * a.C, ch[k], a.C, u + k * VN);
+            ch.load(a.branch, row * a.C, u);
             if (a.gain_branch) {
-                row_stats<TPR, E, LAYER>(u, in, a.inv_c, a.eps, lds[0], st[2], st[3]);
+                row_stats<TPR, E, LAYER>(u, ch, a.inv_c, a.eps, lds[0], st[2], st[3]);
 #pragma unroll
                 for (int e = 0; e < E; ++e) u[e] = (u[e] - st[2]) * st[3];
             }
 #pragma unroll
             for (int e = 0; e < E; ++e) x[e] = (float)(T)fmaf(gz[e], u[e], x[e]);
-#pragma unroll
-            for (int k = 0; k < NV; ++k) n_store(reinterpret_cast<T *>(a.x_out) + row * a.C, ch[k], a.C, x + k * VN);
+            ch.store(a.x_out, row * a.C, x);
         }
         if (a.y) {
-            row_stats<TPR, E, LAYER>(x, in, a.inv_c, a.eps, lds[2], st[0], st[1]);
+            row_stats<TPR, E, LAYER>(x, ch, a.inv_c, a.eps, lds[2], st[0], st[1]);
 #pragma unroll
             for (int e = 0; e < E; ++e) x[e] = fmaf((x[e] - st[0]) * st[1], ga[e], sh[e]);
-#pragma unroll
-            for (int k = 0; k < NV; ++k) n_store(reinterpret_cast<T *>(a.y) + row * a.C, ch[k], a.C, x + k * VN);
+            ch.store(a.y, row * a.C, x);
         }
         if (a.stats && t == 0) *reinterpret_cast<float4 *>(a.stats + 4 * row) = make_float4(st[0], st[1], st[2], st[3]);
         if constexpr (TPR > 64) __syncthreads();             // the next row's sums go where this one's are read
     }
 }
 
-template <class T, int TPR, int NV, bool LAYER>
-__global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormArgs a) {
-    constexpr int VN = NVec<T>::n, E = NV * VN, GP = TPR > 256 ? 1 : 256 / TPR;
+template <class T, int TPR, int NV, bool LAYER, bool FULL>
+__global__ void __launch_bounds__(norm_threads(TPR)) norm_bwd_kernel(NormArgs a) {
+    using Ch = Channels<T, TPR, NV, FULL>;
+    constexpr int E = Ch::E, GP = norm_threads(TPR) / TPR;
     constexpr int SPAN = TPR * E;                            // channels that the threads of a row cover
     __shared__ float lds[2][32];
     __shared__ float sums[GP > 1 ? 3 * SPAN : 1];
     const int t = threadIdx.x % TPR, b = blockIdx.y;
-    int ch[NV];
+    const Ch ch(t, a.C);
     float gz[E], ga[E], sE[E], sT[E], sF[E];
+    channel_factors(a, ch, b * a.mod_stride, gz, ga);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        ch[k] = (k * TPR + t) * VN;
-#pragma unroll
-        for (int e = 0; e < VN; ++e) {
-            const int c = ch[k] + e, i = k * VN + e;
-            const int64_t at = b * a.mod_stride + c;
-            const bool in = c < a.C;
-            gz[i] = in && a.branch ? a.alpha * n_mod(a.gate, a.mod_f32, at, 1.f) * (a.gain_branch ? a.gain_branch[c] : 1.f) : 0.f;
-            ga[i] = in ? (a.gain ? a.gain[c] : 1.f) * (1.f + n_mod(a.scale, a.mod_f32, at, 0.f)) : 0.f;
-            sE[i] = sT[i] = sF[i] = 0.f;
-        }
-    }
-    for (int64_t n = (int64_t)blockIdx.x * GP + threadIdx.x / TPR; n < a.N; n += (int64_t)gridDim.x * GP) {
-        const int64_t row = b * a.N + n, at = row * a.C;
-        float d[E], u[E];                                    // gradient of x'; normed branch
-        const float4 st = *reinterpret_cast<const float4 *>(a.stats + 4 * row);
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] = 0.f;
-        if (a.branch)
-#pragma unroll
-            for (int k = 0; k < NV; ++k) n_load(reinterpret_cast<const T *>(a.branch) + at, ch[k], a.C, u + k * VN);
-        if (a.dx_out)
-#pragma unroll
-            for (int k = 0; k < NV; ++k) n_load(reinterpret_cast<const T *>(a.dx_out) + at, ch[k], a.C, d + k * VN);
+    for (int i = 0; i < E; ++i) sE[i] = sT[i] = sF[i] = 0.f;
+    // The next row is on its way while this one is worked on (32768 rows of 1024: 93 -> 83 us), but where a thousand threads leave no registers
+    // for it. 
+    constexpr bool AHEAD = TPR < 1024;
+    const int64_t step = (int64_t)gridDim.x * GP;
+    int64_t n = (int64_t)blockIdx.x * GP + threadIdx.x / TPR;
+    typename Ch::Raw nx, ny, nb, nd;
+    float4 ns;
+    auto ask = [&](int64_t row) {
+        const int64_t at = row * a.C;
+        ns = *reinterpret_cast<const float4 *>(a.stats + 4 * row);
         if (a.dy) {
-            float x[E], g[E];
+            ch.ask(a.x, at, nx);
+            ch.ask(a.dy, at, ny);
+        }
+        if (a.dx_out) ch.ask(a.dx_out, at, nd);
+        if (a.branch) ch.ask(a.branch, at, nb);
+    };
+    if (AHEAD && n < a.N) ask(b * a.N + n);
+    for (; n < a.N; n += step) {
+        const int64_t row = b * a.N + n, at = row * a.C;
+        float d[E], u[E], x[E], g[E];                        // gradient of x'; normed branch; x', dy
+        if (!AHEAD) ask(row);
+        const float4 st = ns;
+        if (a.dy) {
+            ch.get(nx, x);
+            ch.get(ny, g);
+        }
+        if (a.branch) ch.get(nb, u);
+        if (a.dx_out) {
+            ch.get(nd, d);
+        } else {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) n_load(reinterpret_cast<const T *>(a.x) + at, ch[k], a.C, x + k * VN);
-#pragma unroll
-            for (int k = 0; k < NV; ++k) n_load(reinterpret_cast<const T *>(a.dy) + at, ch[k], a.C, g + k * VN);
+            for (int e = 0; e < E; ++e) d[e] = 0.f;
+        }
+        if (AHEAD && n + step < a.N) ask(row + step);
+        if (a.dy) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                x[e] = (x[e] - st.x) * st.y;                 // beyond C: a value that only meets zeros
+                x[e] = (x[e] - st.x) * st.y;                 // not its own: a value that only meets zeros
                 sE[e] = fmaf(g[e], x[e], sE[e]);
                 sT[e] += g[e];
                 g[e] *= ga[e];
@@ -231,8 +302,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormArg
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] = fmaf(st.y, fmaf(-x[e], m[0], g[e]) - m[1], d[e]);
         }
-#pragma unroll
-        for (int k = 0; k < NV; ++k) n_store(reinterpret_cast<T *>(a.dx) + at, ch[k], a.C, d + k * VN);
+        ch.store(a.dx, at, d);
         if (a.branch) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
@@ -256,8 +326,7 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormArg
 #pragma unroll
                 for (int e = 0; e < E; ++e) d[e] = (fmaf(-u[e], m[0], d[e]) - m[1]) * st.w;
             }
-#pragma unroll
-            for (int k = 0; k < NV; ++k) n_store(reinterpret_cast<T *>(a.dbranch) + at, ch[k], a.C, d + k * VN);
+            ch.store(a.dbranch, at, d);
         }
         if constexpr (TPR > 64) __syncthreads();             // the next row's sums go where this one's are read
     }
@@ -287,59 +356,77 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) norm_bwd_kernel(NormArg
     }
     float *part = a.part + ((int64_t)b * gridDim.x + blockIdx.x) * 3 * a.C;
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < VN; ++e) {
-            const int c = ch[k] + e, i = k * VN + e;
-            if (c < a.C) {
-                part[c] = sE[i];
-                part[a.C + c] = sT[i];
-                part[2 * a.C + c] = sF[i];
-            }
+    for (int i = 0; i < E; ++i) {
+        const int c = ch.channel(i);
+        if (ch.mine(i)) {
+            part[c] = sE[i];
+            part[a.C + c] = sT[i];
+            part[2 * a.C + c] = sF[i];
         }
+    }
 }
 
-// The workgroups' sums added up: 16 slices of 64 channels a workgroup, each slice every 16th workgroup's, then the slices in order.
+// The workgroups' sums added up: 64 slices of 16 channels a workgroup, each slice every 64th workgroup's, then the slices in order.
 __global__ void __launch_bounds__(1024) norm_sums_kernel(NormArgs a) {
-    __shared__ float lds[3][16][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
+    __shared__ float lds[3][64][17];
+    const int col = threadIdx.x & 15, c = blockIdx.x * 16 + col, slice = threadIdx.x >> 4;
     const bool in = c < a.C;
     float dgain = 0.f, dgb = 0.f, shared[3] = {0.f, 0.f, 0.f};
     const float gain = in && a.gain ? a.gain[c] : 1.f, gb = in && a.gain_branch ? a.gain_branch[c] : 1.f;
-    for (int b = 0; b < a.batch; ++b) {
-        float s[3] = {0.f, 0.f, 0.f};
-        if (in)
-            for (int w = slice; w < a.blocks; w += 16) {
-                const float *p = a.part + ((int64_t)b * a.blocks + w) * 3 * a.C + c;
+    for (int b0 = 0; b0 < a.batch; b0 += 2) {                // two batch entries' and eight workgroups' sums on their way at once
+        float s[2][3] = {};
+        if (in) {
+            for (int w0 = slice; w0 < a.blocks; w0 += 512) {
+                float v[8][2][3];
 #pragma unroll
-                for (int k = 0; k < 3; ++k) s[k] += p[k * a.C];
-            }
+                for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int k = 0; k < 3; ++k) lds[k][slice][threadIdx.x & 63] = s[k];
-        __syncthreads();
-        if (slice == 0 && in) {
-            float v[3];
+                    for (int i = 0; i < 2; ++i) {
+                        const float *p = a.part + ((int64_t)min(b0 + i, a.batch - 1) * a.blocks + min(w0 + 64 * j, a.blocks - 1)) * 3 * a.C + c;
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                v[k] = 0.f;
+                        for (int k = 0; k < 3; ++k) v[j][i][k] = p[k * a.C];
+                    }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[k] += lds[k][i][threadIdx.x];
-            }
-            const int64_t at = b * a.mod_stride + c;
-            dgain = fmaf(1.f + n_mod(a.scale, a.mod_f32, at, 0.f), v[0], dgain);
-            dgb = fmaf(a.alpha * n_mod(a.gate, a.mod_f32, at, 1.f), v[2], dgb);
+                for (int j = 0; j < 8; ++j)
 #pragma unroll
-            for (int k = 0; k < 3; ++k) shared[k] += v[k];
-            if (a.mod_stride || b == a.batch - 1) {
-                const int64_t to = (a.mod_stride ? (int64_t)b * a.C : 0) + c;
-                if (a.dscale) a.dscale[to] = gain * shared[0];
-                if (a.dshift) a.dshift[to] = shared[1];
-                if (a.dgate) a.dgate[to] = a.alpha * gb * shared[2];
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int k = 0; k < 3; ++k) shared[k] = 0.f;
+                        for (int k = 0; k < 3; ++k) s[i][k] += w0 + 64 * j < a.blocks ? v[j][i][k] : 0.f;
             }
         }
-        __syncthreads();
+        for (int i = 0; i < 2 && b0 + i < a.batch; ++i) {
+            const int b = b0 + i;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) lds[k][slice][col] = i == 0 ? s[0][k] : s[1][k];
+            __syncthreads();
+            if (slice < 4) {                                 // 16 slices each, then those four
+                float v[3];
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    v[k] = 0.f;
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) v[k] += lds[k][slice * 16 + q][col];
+                    v[k] += __shfl_xor(v[k], 16, 64);
+                    v[k] += __shfl_xor(v[k], 32, 64);
+                }
+                if (slice == 0 && in) {
+                    const int64_t at = b * a.mod_stride + c;
+                    dgain = fmaf(1.f + n_mod(a.scale, a.mod_f32, at, 0.f), v[0], dgain);
+                    dgb = fmaf(a.alpha * n_mod(a.gate, a.mod_f32, at, 1.f), v[2], dgb);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) shared[k] += v[k];
+                    if (a.mod_stride || b == a.batch - 1) {
+                        const int64_t to = (a.mod_stride ? (int64_t)b * a.C : 0) + c;
+                        if (a.dscale) a.dscale[to] = gain * shared[0];
+                        if (a.dshift) a.dshift[to] = shared[1];
+                        if (a.dgate) a.dgate[to] = a.alpha * gb * shared[2];
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) shared[k] = 0.f;
+                    }
+                }
+            }
+            __syncthreads();
+        }
     }
     if (slice == 0 && in) {
         if (a.dgain) a.dgain[c] = dgain;
@@ -347,36 +434,50 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(NormArgs a) {
     }
 }
 
-// The fewest threads a row that hold it with at most 16 channels each.
+// The fewest threads a row that hold it with at most `most` channels each, 4 to 64 or whole waves.
+static NormShape norm_shape(const llsa_norm_desc &d, int most, int64_t target) {
+    NormShape r;
+    const int vn = d.dtype == LLSA_F32 ? 4 : 8, vec = (d.C + vn - 1) / vn, nv = most / vn;
+    r.tpr = vec <= 16 ? 16 : 64;
+    while (vec > r.tpr * nv) r.tpr *= 2;
+    r.nv = (vec + r.tpr - 1) / r.tpr;
+    if (r.nv == 3) r.nv = 4;
+    const int64_t rows = norm_threads(r.tpr) / r.tpr, all = (d.N + rows - 1) / rows, share = (target * 256 / norm_threads(r.tpr) + d.batch - 1) / d.batch;
+    r.blocks = (int)(all < share ? all : share);
+    return r;
+}
 void norm_layout(NormPlan &p) {
-    const llsa_norm_desc &d = p.desc;
-    const int vn = d.dtype == LLSA_F32 ? 4 : 8, vec = (d.C + vn - 1) / vn, most = 16 / vn;
-    p.tpr = vec <= 16 ? 16 : vec <= 64 * 2 ? 64 : vec <= 256 * most ? 256 : 512;
-    p.nv = (vec + p.tpr - 1) / p.tpr;
-    if (p.nv == 3) p.nv = 4;
-    const int64_t groups = p.tpr >= 256 ? 1 : 256 / p.tpr, all = (d.N + groups - 1) / groups;
-    auto blocks = [&](int64_t target) {
-        target = (target + d.batch - 1) / d.batch;
-        return (int)(all < target ? all : target);
-    };
-    p.fwd_blocks = blocks(2048);
-    p.bwd_blocks = blocks(1024);
-    p.ws = (size_t)d.batch * p.bwd_blocks * 3 * d.C * sizeof(float);
+    p.fwd = norm_shape(p.desc, 16, 1024);
+    p.bwd = norm_shape(p.desc, 8, 512);
+    p.ws = (size_t)p.desc.batch * p.bwd.blocks * 3 * p.desc.C * sizeof(float);
 }
 
-template <class F> static void norm_dispatch(const NormPlan &p, F go) {
+// As norm_layout chooses: at most 16 channels a thread, 8 in the backward pass
+template <bool FWD, class F> static void norm_dispatch(const NormPlan &p, const NormShape &sh, F go) {
+    using std::integral_constant;
     auto shape = [&](auto t, auto layer) {
-        auto with = [&](auto tpr, auto nv) { go(t, tpr, nv, layer); };
-        using std::integral_constant;
-        auto wide = [&](auto tpr) {
-            if (p.nv == 1) with(tpr, integral_constant<int, 1>());
-            else if (p.nv == 2 || sizeof(t) == 2) with(tpr, integral_constant<int, 2>());
-            else if constexpr (sizeof(t) == 4) with(tpr, integral_constant<int, 4>());
+        constexpr int vn = 16 / sizeof(t);
+        auto with = [&](auto tpr, auto nv) {
+            if (p.desc.C == sh.tpr * sh.nv * vn) go(t, tpr, nv, layer, std::true_type());
+            else go(t, tpr, nv, layer, std::false_type());
         };
-        if (p.tpr == 16) with(integral_constant<int, 16>(), integral_constant<int, 1>());
-        else if (p.tpr == 64) wide(integral_constant<int, 64>());
-        else if (p.tpr == 256) wide(integral_constant<int, 256>());
-        else wide(integral_constant<int, 512>());
+        auto wide = [&](auto tpr) {
+            constexpr int most = (FWD ? 16 : 8) / vn;
+            if (sh.nv == 1) with(tpr, integral_constant<int, 1>());
+            else if constexpr (most >= 2) {
+                if (sh.nv == 2) with(tpr, integral_constant<int, 2>());
+                else if constexpr (most >= 4) with(tpr, integral_constant<int, 4>());
+            }
+        };
+        switch (sh.tpr) {
+            case 16: with(integral_constant<int, 16>(), integral_constant<int, 1>()); break;
+            case 64: wide(integral_constant<int, 64>()); break;
+            case 128: wide(integral_constant<int, 128>()); break;
+            case 256: wide(integral_constant<int, 256>()); break;
+            case 512: wide(integral_constant<int, 512>()); break;
+            default:
+                if constexpr (!FWD) wide(integral_constant<int, 1024>());
+        }
     };
     auto kind = [&](auto t) {
         if (p.desc.kind == LLSA_NORM_LAYER) shape(t, std::true_type());
@@ -387,24 +488,24 @@ template <class F> static void norm_dispatch(const NormPlan &p, F go) {
 }
 
 hipError_t launch_norm_forward(const NormPlan &p, NormArgs a, hipStream_t s) {
-    const dim3 grid(p.fwd_blocks, p.desc.batch);
-    norm_dispatch(p, [&](auto t, auto tpr, auto nv, auto layer) {
-        constexpr int threads = decltype(tpr)::value > 256 ? decltype(tpr)::value : 256;
-        norm_fwd_kernel<decltype(t), decltype(tpr)::value, decltype(nv)::value, decltype(layer)::value><<<grid, threads, 0, s>>>(a);
+    const dim3 grid(p.fwd.blocks, p.desc.batch);
+    norm_dispatch<true>(p, p.fwd, [&](auto t, auto tpr, auto nv, auto layer, auto full) {
+        constexpr int threads = norm_threads(decltype(tpr)::value);
+        norm_fwd_kernel<decltype(t), decltype(tpr)::value, decltype(nv)::value, decltype(layer)::value, decltype(full)::value><<<grid, threads, 0, s>>>(a);
     });
     return hipGetLastError();
 }
 
 hipError_t launch_norm_backward(const NormPlan &p, NormArgs a, hipStream_t s) {
-    const dim3 grid(p.bwd_blocks, p.desc.batch);
-    a.blocks = p.bwd_blocks;
-    norm_dispatch(p, [&](auto t, auto tpr, auto nv, auto layer) {
-        constexpr int threads = decltype(tpr)::value > 256 ? decltype(tpr)::value : 256;
-        norm_bwd_kernel<decltype(t), decltype(tpr)::value, decltype(nv)::value, decltype(layer)::value><<<grid, threads, 0, s>>>(a);
+    const dim3 grid(p.bwd.blocks, p.desc.batch);
+    a.blocks = p.bwd.blocks;
+    norm_dispatch<false>(p, p.bwd, [&](auto t, auto tpr, auto nv, auto layer, auto full) {
+        constexpr int threads = norm_threads(decltype(tpr)::value);
+        norm_bwd_kernel<decltype(t), decltype(tpr)::value, decltype(nv)::value, decltype(layer)::value, decltype(full)::value><<<grid, threads, 0, s>>>(a);
     });
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
-    norm_sums_kernel<<<(a.C + 63) / 64, 1024, 0, s>>>(a);
+    norm_sums_kernel<<<(a.C + 15) / 16, 1024, 0, s>>>(a);
     return hipGetLastError();
 }
 
