@@ -12,6 +12,13 @@ namespace llsa {
 
 struct DenseStrides { int64_t batch, head, token; };     // bytes
 
+// How a launch cuts its axis (rows, or keys) and the other one that each tile of it walks over
+struct DenseShape {
+    bool narrow;                    // tiles of 32, whose four waves share out the other axis among themselves; else of 128, 32 a wave
+    int splits;                     // workgroups that share out the other axis beyond that
+    int chunk;                      // .. in pieces of this many of its tiles: a tile that sees less of it has fewer workgroups with something to do
+};
+
 struct DensePlan {
     llsa_dense_desc desc;
     int elt, G;                     // bytes per element, query heads per key head
@@ -19,7 +26,7 @@ struct DensePlan {
     float scale;
     DenseStrides q, k, v, o;
     bool grads;                     // may gradients be written with the strides of Q, K and V?
-    int fwd_splits, dq_splits, dkv_splits;     // workgroups that share out the other axis of a tile of rows or keys
+    DenseShape fwd, dq, dkv;
     int64_t stat_rows;              // rows, rounded up to whole tiles
     size_t nD_off, nlse_off;        // backward: -D = -rowsum(dO * O) and -LSE / scale of the rows of a group, [batch * kv_heads, stat_rows] fp32
     size_t part_off;                // backward: partial sums of split tiles
@@ -30,7 +37,7 @@ struct DensePlan {
 struct DenseGrid {
     FastDiv by_tiles, by_splits, by_rest;      // rest: groups x splits
     uint32_t wgs, groups;
-    int32_t splits;
+    int32_t splits, chunk;
     int64_t rows;                   // rows (or keys) of a group
     float *part, *stat;             // [split][group][row][d] partial sums; [split][group][row][2] their references and sums
 };
@@ -59,14 +66,14 @@ template <class F> auto dense_dispatch(const DensePlan &p, F go) {
     };
     return p.elt == 4 ? by_d(float()) : by_d(__bf16());
 }
-DenseGrid dense_grid(const DensePlan &p, int64_t rows, int tile, int splits, int row_floats, float *part);
-size_t dense_part_bytes(const DensePlan &p, int64_t rows, int splits, int row_floats);
+constexpr int dense_tile(bool narrow) { return narrow ? 32 : 128; }                                       // of the launch's axis
+constexpr int dense_step(int row_bytes, bool narrow) { return narrow || row_bytes > 256 ? 32 : 64; }      // of the other one
+DenseShape dense_shape(const DensePlan &p, int64_t axis, int64_t other);
+DenseGrid dense_grid(const DensePlan &p, int64_t rows, const DenseShape &shape, int row_floats, float *part);
+size_t dense_part_bytes(const DensePlan &p, int64_t rows, const DenseShape &shape, int row_floats);
 
 // tiles on the matrix instructions (dense_fwd.hip, dense_bwd.hip)
-int dense_fwd_splits(const DensePlan &p);
 hipError_t launch_dense_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s);
-int dense_dq_splits(const DensePlan &p);
-int dense_dkv_splits(const DensePlan &p);
 hipError_t launch_dense_bwd(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s);
 
 // one wave a row (dense_row.hip)

@@ -38,6 +38,45 @@ static bool dense_apart(const DenseStrides &st, int64_t batch, int64_t heads, in
     return true;
 }
 
+// Tiles of 128 rows, each wave 32 of them, keep the matrix units busiest (the other axis is brought in once for all four); tiles of 32, whose waves share out the
+// other axis, are for what leaves half a tile or half the CUs empty otherwise.  The other axis is cut where there are fewer tiles than the CUs hold (two
+// workgroups each), not into pieces of less than 512 rows or keys: the partial sums are written and read once more.  Causal tiles differ, and the longest
+// alone takes as long as everything where all are resident at once; long ones are cut up to twice as many tiles (d = 64, 4 heads x 16384: 298 -> 243 us;
+// 16 x 4096, 64 steps of 64 keys, 74 -> 87).
+DenseShape dense_shape(const DensePlan &p, int64_t axis, int64_t other) {
+    DenseShape r;
+    const int64_t groups = (int64_t)p.desc.batch * p.desc.kv_heads, wide = groups * ((axis + 127) / 128), pieces = std::max<int64_t>(1, other / 512);
+    r.narrow = axis <= 64 || wide * pieces < 128;
+    const int step = dense_step(p.desc.d * p.elt, r.narrow);
+    const int64_t tiles = r.narrow ? groups * ((axis + 31) / 32) : wide, steps = (other + step - 1) / step, least = 512 / step;
+    const bool differ = p.desc.causal && !r.narrow;
+    const int64_t target = differ && steps >= 128 ? 1024 : 512, want = tiles >= (differ ? target : 256) ? 1 : (target + tiles - 1) / tiles;
+    r.chunk = (int)std::max((steps + want - 1) / want, least);
+    r.splits = (int)((steps + r.chunk - 1) / r.chunk);
+    return r;
+}
+
+DenseGrid dense_grid(const DensePlan &p, int64_t rows, const DenseShape &shape, int row_floats, float *part) {
+    DenseGrid g;
+    memset(&g, 0, sizeof(g));
+    g.rows = rows;
+    g.groups = (uint32_t)(p.desc.batch * p.desc.kv_heads);
+    g.splits = shape.splits;
+    g.chunk = shape.chunk;
+    const int64_t tile = dense_tile(shape.narrow), tiles = (rows + tile - 1) / tile;
+    g.by_tiles = FastDiv(tiles);
+    g.by_splits = FastDiv(g.splits);
+    g.by_rest = FastDiv((int64_t)g.groups * g.splits);
+    g.wgs = (uint32_t)(tiles * g.groups * g.splits);
+    g.part = part;
+    if (g.splits > 1) g.stat = part + (int64_t)g.splits * g.groups * rows * row_floats;
+    return g;
+}
+
+size_t dense_part_bytes(const DensePlan &p, int64_t rows, const DenseShape &shape, int row_floats) {
+    return shape.splits == 1 ? 0 : dense_align((size_t)shape.splits * p.desc.batch * p.desc.kv_heads * rows * row_floats * sizeof(float));
+}
+
 static llsa_status build_dense_plan(const llsa_dense_desc &d, DensePlan &p) {
     memset(&p, 0, sizeof(p));
     p.desc = d;
@@ -68,37 +107,20 @@ static llsa_status build_dense_plan(const llsa_dense_desc &d, DensePlan &p) {
         if (256 * p.k.token > most || 256 * p.v.token > most || (p.G - 1) * p.q.head + 256 * p.q.token > most || (p.G - 1) * p.o.head + 256 * p.o.token > most)
             return LLSA_ERR_UNSUPPORTED;
     }
-    p.fwd_splits = d.kernel_path ? 1 : dense_fwd_splits(p);
-    p.dq_splits = d.kernel_path ? 1 : dense_dq_splits(p);
-    p.dkv_splits = d.kernel_path ? 1 : dense_dkv_splits(p);
-    p.ws_fwd = dense_part_bytes(p, p.rows, p.fwd_splits, d.d + 2);
+    if (d.kernel_path == 0) {
+        p.fwd = p.dq = dense_shape(p, p.rows, d.Nkv);
+        p.dkv = dense_shape(p, d.Nkv, p.rows);
+    } else {
+        p.fwd.splits = p.dq.splits = p.dkv.splits = 1;
+    }
+    p.ws_fwd = dense_part_bytes(p, p.rows, p.fwd, d.d + 2);
     p.stat_rows = (p.rows + 127) / 128 * 128;
     const size_t stat = dense_align((size_t)d.batch * d.kv_heads * p.stat_rows * sizeof(float));
     p.nD_off = 0;
     p.nlse_off = stat;
     p.part_off = 2 * stat;
-    p.ws_bwd = p.part_off + std::max(dense_part_bytes(p, p.rows, p.dq_splits, d.d), dense_part_bytes(p, d.Nkv, p.dkv_splits, 2 * d.d));
+    p.ws_bwd = p.part_off + std::max(dense_part_bytes(p, p.rows, p.dq, d.d), dense_part_bytes(p, d.Nkv, p.dkv, 2 * d.d));
     return LLSA_OK;
-}
-
-DenseGrid dense_grid(const DensePlan &p, int64_t rows, int tile, int splits, int row_floats, float *part) {
-    DenseGrid g;
-    memset(&g, 0, sizeof(g));
-    g.rows = rows;
-    g.groups = (uint32_t)(p.desc.batch * p.desc.kv_heads);
-    g.splits = splits;
-    const int64_t tiles = (rows + tile - 1) / tile;
-    g.by_tiles = FastDiv(tiles);
-    g.by_splits = FastDiv(splits);
-    g.by_rest = FastDiv((int64_t)g.groups * splits);
-    g.wgs = (uint32_t)(tiles * g.groups * splits);
-    g.part = part;
-    if (splits > 1) g.stat = part + (int64_t)splits * g.groups * rows * row_floats;
-    return g;
-}
-
-size_t dense_part_bytes(const DensePlan &p, int64_t rows, int splits, int row_floats) {
-    return splits == 1 ? 0 : dense_align((size_t)splits * p.desc.batch * p.desc.kv_heads * rows * row_floats * sizeof(float));
 }
 
 static DenseArgs dense_args(const DensePlan &p, const void *Q, const void *K, const void *V, const int32_t *q_lens, const int32_t *kv_lens, float *LSE) {

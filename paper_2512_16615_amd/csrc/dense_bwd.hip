@@ -8,20 +8,24 @@
 
 namespace llsa {
 
-template <class T, int D> constexpr int bwd_waves() { return D * (int)sizeof(T) <= 256 ? 2 : 1; }
+// waves a SIMD that the registers are shared out for (a narrow workgroup's rings take all of a CU's LDS at 256 bytes a row)
+template <class T, int D, bool NARROW> constexpr int bwd_waves() { return D * (int)sizeof(T) <= (NARROW ? 128 : 256) ? 2 : 1; }
 
-template <class T, int D, int KT>
-__global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dq_kernel(DenseArgs a, DenseGrid grid) {
+// NARROW: 32 rows a workgroup, of which each wave has every fourth tile of keys, in stages of its own; the waves' sums are added up at the end.
+template <class T, int D, int KT, bool NARROW>
+__global__ void __launch_bounds__(256, (bwd_waves<T, D, NARROW>())) dense_dq_kernel(DenseArgs a, DenseGrid grid) {
     using Tile = DenseTile<T, D>;
-    using Loads = TileLoads<T, D, KT, 4>;
-    constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][TILEB];      // stage; keys, values
+    using Loads = TileLoads<T, D, KT, NARROW ? 1 : 4>;
+    constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1;
+    constexpr int ST = dense_stages<T, D, NARROW>(), LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * Tile::NB : 0;
+    __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];      // wave; stage; keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const DenseWork work = dense_work(grid, a.causal, true);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
-    const int64_t row0 = (int64_t)work.tile * 128, wrow0 = row0 + wave * 32, r = wrow0 + col;
-    const int end = key_span(a, p, row0, row0 + 127).some;
+    const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + wave * 32, r = wrow0 + col;
+    const DensePieces piece(grid, work.split, 0, dense_key_steps<AXIS, KT>(a, p, row0));
+    if (piece.none) return;
     const KeySpan mine = key_span(a, p, wrow0, wrow0 + 31);
 
     const bool in = r < grid.rows;
@@ -38,7 +42,7 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dq_kernel(Dens
         delta = piece_dot(g[ks], o, delta);
     }
     const float nD = -half_sum(delta), nlse = seen > 0 ? -p.LSE[(int64_t)qg * a.Nq + qi] / a.scale : -INFINITY;
-    if (work.split == 0 && h == 0) {                         // also for the rows that the last tile has too many
+    if (work.split == 0 && h == 0 && (!NARROW || wave == 0)) {                         // also for the rows that the last tile has too many
         a.nD[work.group * a.stat_rows + r] = nD;
         a.nlse[work.group * a.stat_rows + r] = nlse;
     }
@@ -51,29 +55,37 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dq_kernel(Dens
         for (int n = 0; n < Tile::NB; ++n) dq[n][e] = 0.f;
     }
 
-    const int tiles = (end + KT - 1) / KT, per = (tiles + grid.splits - 1) / grid.splits;
-    const int t0 = work.split * per, t1 = min(tiles, t0 + per);
+    char *const ring = lds + (NARROW ? wave * (ST * 2 * TILEB) : 0);
+    const unsigned ring0 = lds_address(ring);
+    const int t0 = piece.t0 + (NARROW ? wave : 0);
+    auto stage = [&](int t) { return ST == 1 ? 0 : ((t - t0) / WAVES & 1) * 2 * TILEB; };
     auto fetch = [&](int t) {
         const int k0 = t * KT, left = min(KT, p.nk - k0);
-        const unsigned lds0 = lds_address(&lds[t & 1][0][0]);
-        const unsigned kt = (unsigned)a.k.token, vt = (unsigned)a.v.token;
-        Loads::keys(buffer_of(p.K + k0 * a.k.token, (left - 1) * kt + Tile::ROWB), kt, lds0, wave, lane);
-        Loads::keys(buffer_of(p.V + k0 * a.v.token, (left - 1) * vt + Tile::ROWB), vt, lds0 + TILEB, wave, lane);
+        const unsigned kt = (unsigned)a.k.token, vt = (unsigned)a.v.token, to = ring0 + stage(t);
+        Loads::keys(buffer_of(p.K + k0 * a.k.token, (left - 1) * kt + Tile::ROWB), kt, to, NARROW ? 0 : wave, lane);
+        Loads::keys(buffer_of(p.V + k0 * a.v.token, (left - 1) * vt + Tile::ROWB), vt, to + TILEB, NARROW ? 0 : wave, lane);
     };
-    if (t0 < t1) fetch(t0);
-    for (int t = t0; t < t1; ++t) {
-        vm_wait_barrier<0>();                                // tile t is there, and nobody reads the other stage
-        if (t + 1 < t1) fetch(t + 1);
+    if (ST == 2 && t0 < piece.t1) fetch(t0);
+    loads_done();
+    for (int t = t0; t < piece.t1; t += WAVES) {
+        if (ST == 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            fetch(t);
+        }
+        if (NARROW) vm_wait<0>();                            // tile t is there (and nobody else reads the wave's stages),
+        else vm_wait_barrier<0>();                           // for all waves, and nobody reads the other stage
+        if (ST == 2 && t + WAVES < piece.t1) fetch(t + WAVES);
         const int k0 = t * KT;
         if (k0 >= mine.some) continue;
-        const char *kt = &lds[t & 1][0][0], *vt = &lds[t & 1][1][0];
-#pragma unroll
-        for (int u = 0; u < SUBS; ++u) {
+        const char *kt = ring, *vt = ring + TILEB;
+#pragma unroll 1
+        for (int u = 0; u < SUBS; ++u) {                     // (unrolled, the operands of two of them at once do not fit at d = 128)
+            const Tile at = tile.at(stage(t) + u * 32 * Tile::ROWB);
             f32x16 s = s_from, dp = dp_from;
 #pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(tile.row(kt, u, ks), q[ks], s);
+            for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(at.row(kt, 0, ks), q[ks], s);
 #pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(tile.row(vt, u, ks), g[ks], dp);
+            for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(vt, 0, ks), g[ks], dp);
 #pragma unroll
             for (int e = 0; e < 16; ++e) dp[e] *= __builtin_amdgcn_exp2f(s[e] * a.scale2);
             if (k0 + 32 * u + 32 > mine.all) {
@@ -84,11 +96,16 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dq_kernel(Dens
             Probs<T> ds;
             ds.set(dp);
 #pragma unroll
-            for (int n = 0; n < Tile::NB; ++n) dq[n] = tile.col_product(kt, u, n, ds, dq[n]);
+            for (int n = 0; n < Tile::NB; ++n) dq[n] = at.col_product(kt, 0, n, ds, dq[n]);
         }
     }
 
-    if (grid.splits > 1) {
+    if constexpr (NARROW) {
+        __syncthreads();
+        add_waves(dq, 1.f, lds, wave, lane);
+        if (wave > 0) return;
+    }
+    if (!piece.alone) {
         if (in) store_partial<D>(grid.part + (((int64_t)work.split * grid.groups + work.group) * grid.rows + r) * D, dq, h);
         return;
     }
@@ -107,18 +124,25 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dq_kernel(Dens
 }
 
 // A wave has 32 keys, theirs and their values' channels in registers, and walks over the rows (of every head that shares them) in tiles of QT.
-template <class T, int D, int QT>
-__global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dkv_kernel(DenseArgs a, DenseGrid grid) {
+// NARROW: 32 keys a workgroup, for which each wave has every fourth tile of rows, in stages of its own.
+template <class T, int D, int QT, bool NARROW>
+__global__ void __launch_bounds__(256, (bwd_waves<T, D, NARROW>())) dense_dkv_kernel(DenseArgs a, DenseGrid grid) {
     using Tile = DenseTile<T, D>;
-    using Loads = TileLoads<T, D, QT, 4>;
-    constexpr int TILEB = QT * Tile::ROWB, SUBS = QT / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][TILEB];      // stage; queries, their output's gradients
-    __shared__ __attribute__((aligned(1024))) float stat[2][2][64];       // stage; -LSE / scale, -D
+    using Loads = TileLoads<T, D, QT, NARROW ? 1 : 4>;
+    constexpr int TILEB = QT * Tile::ROWB, SUBS = QT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1;
+    constexpr int ST = dense_stages<T, D, NARROW>(), STAGEB = 2 * TILEB + 1024;
+    constexpr int LDSB = WAVES * ST * STAGEB, JOINB = NARROW ? 24576 * Tile::NB : 0;
+    // wave; stage; queries, their output's gradients, their -LSE / scale and -D
+    __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const DenseWork work = dense_work(grid, a.causal, false);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
-    const int key0 = work.tile * 128, wkey0 = key0 + wave * 32, j = wkey0 + col;
+    const int key0 = work.tile * AXIS, wkey0 = NARROW ? key0 : key0 + wave * 32, j = wkey0 + col;
+    int first;
+    const int steps = dense_row_steps<QT>(a, p, key0, &first);
+    const DensePieces piece(grid, work.split, first, steps);
+    if (piece.none) return;
     const bool valid = j < p.nk;
 
     Piece<T> k[Tile::KS], v[Tile::KS];
@@ -137,26 +161,35 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dkv_kernel(Den
     const int rows = p.nq * a.G;                             // rows that see something: of each key, those from its first query's on
     const int from = p.first_query(a, j) * a.G;
     const int wfrom = p.first_query(a, wkey0) * a.G, wto = p.first_query(a, min(wkey0 + 31, max(p.nk - 1, 0))) * a.G;
-    const int first = p.first_query(a, key0) * a.G / QT, tiles = max(0, (rows + QT - 1) / QT - first), per = (tiles + grid.splits - 1) / grid.splits;
-    const int t0 = first + work.split * per, t1 = min(first + tiles, t0 + per);
     const float *nlse = a.nlse + work.group * a.stat_rows, *nD = a.nD + work.group * a.stat_rows;
+    char *const ring = lds + (NARROW ? wave * (ST * STAGEB) : 0);
+    const unsigned ring0 = lds_address(ring);
+    const int t0 = piece.t0 + (NARROW ? wave : 0);
+    auto stage = [&](int t) { return ST == 1 ? 0 : ((t - t0) / WAVES & 1) * STAGEB; };
     auto fetch = [&](int t) {
         const int r0 = t * QT, q0 = (int)a.div_g(r0);
-        const unsigned lds0 = lds_address(&lds[t & 1][0][0]), st0 = lds_address(&stat[t & 1][0][0]);
-        Loads::rows(buffer_of(p.Q + (int64_t)q0 * a.q.token, 0xffffff00u), buffer_of(p.dO + (int64_t)q0 * a.o.token, 0xffffff00u), a, r0, q0, rows, lds0, lds0 + TILEB, wave, lane);
-        const float *src = wave == 0 ? nlse : nD;
-        if (wave < 2) buffer_to_lds_dword(buffer_of(reinterpret_cast<const char *>(src + r0), (unsigned)min((int64_t)64, a.stat_rows - r0) * 4), lane * 4, st0 + wave * 256);
+        const unsigned to = ring0 + stage(t), st0 = to + 2 * TILEB, bytes = (unsigned)min((int64_t)64, a.stat_rows - r0) * 4;
+        Loads::rows(buffer_of(p.Q + (int64_t)q0 * a.q.token, 0xffffff00u), buffer_of(p.dO + (int64_t)q0 * a.o.token, 0xffffff00u), a, r0, q0, rows, to, to + TILEB, NARROW ? 0 : wave, lane);
+        if (NARROW || wave == 0) buffer_to_lds_dword(buffer_of(reinterpret_cast<const char *>(nlse + r0), bytes), lane * 4, st0);
+        if (NARROW || wave == 1) buffer_to_lds_dword(buffer_of(reinterpret_cast<const char *>(nD + r0), bytes), lane * 4, st0 + 256);
     };
-    if (t0 < t1) fetch(t0);
-    for (int t = t0; t < t1; ++t) {
-        vm_wait_barrier<0>();                                // tile t is there, and nobody reads the other stage
-        if (t + 1 < t1) fetch(t + 1);
-        const char *qt = &lds[t & 1][0][0], *gt = &lds[t & 1][1][0];
-        const float *st = &stat[t & 1][0][0];
-#pragma unroll
+    if (ST == 2 && t0 < piece.t1) fetch(t0);
+    loads_done();
+    for (int t = t0; t < piece.t1; t += WAVES) {
+        if (ST == 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            fetch(t);
+        }
+        if (NARROW) vm_wait<0>();                            // tile t is there (and nobody else reads the wave's stages),
+        else vm_wait_barrier<0>();                           // for all waves, and nobody reads the other stage
+        if (ST == 2 && t + WAVES < piece.t1) fetch(t + WAVES);
+        const char *qt = ring, *gt = ring + TILEB;
+        const float *st = reinterpret_cast<const float *>(ring + stage(t) + 2 * TILEB);
+#pragma unroll 1
         for (int u = 0; u < SUBS; ++u) {
             const int r0 = t * QT + 32 * u;
             if (r0 + 31 < wfrom) continue;
+            const Tile at = tile.at(stage(t) + u * 32 * Tile::ROWB);
             f32x16 s, dp;
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
@@ -165,9 +198,9 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dkv_kernel(Den
                 for (int i = 0; i < 4; ++i) { s[e + i] = x[i]; dp[e + i] = y[i]; }
             }
 #pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(tile.row(qt, u, ks), k[ks], s);
+            for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(at.row(qt, 0, ks), k[ks], s);
 #pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(tile.row(gt, u, ks), v[ks], dp);
+            for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(gt, 0, ks), v[ks], dp);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 s[e] = __builtin_amdgcn_exp2f(s[e] * a.scale2);
@@ -186,13 +219,19 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dkv_kernel(Den
             pr.set(s);
             ds.set(dp);
 #pragma unroll
-            for (int n = 0; n < Tile::NB; ++n) dv[n] = tile.col_product(gt, u, n, pr, dv[n]);
+            for (int n = 0; n < Tile::NB; ++n) dv[n] = at.col_product(gt, 0, n, pr, dv[n]);
 #pragma unroll
-            for (int n = 0; n < Tile::NB; ++n) dk[n] = tile.col_product(qt, u, n, ds, dk[n]);
+            for (int n = 0; n < Tile::NB; ++n) dk[n] = at.col_product(qt, 0, n, ds, dk[n]);
         }
     }
 
-    if (grid.splits > 1) {
+    if constexpr (NARROW) {
+        __syncthreads();
+        add_waves(dk, 1.f, lds, wave, lane);
+        add_waves(dv, 1.f, lds + 12288 * Tile::NB, wave, lane);
+        if (wave > 0) return;
+    }
+    if (!piece.alone) {
         float *to = grid.part + (((int64_t)work.split * grid.groups + work.group) * grid.rows + j) * (2 * D);
         if (j < grid.rows) {
             store_partial<D>(to, dk, h);
@@ -216,31 +255,36 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D>())) dense_dkv_kernel(Den
     }
 }
 
-// The splits' sums of a row in order, one wave a row.
-template <class T, int D> __global__ void __launch_bounds__(256) dense_dq_join_kernel(DenseArgs a, DenseGrid grid) {
+// The pieces' sums of a row in order, one wave a row; where there was one piece, its sums are the result already.
+template <class T, int D, int AXIS, int KT> __global__ void __launch_bounds__(256) dense_dq_join_kernel(DenseArgs a, DenseGrid grid) {
     using Row = LaneRow<T, D>;
     const int lane = threadIdx.x & 63;
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= grid.rows) return;
     const DenseGroup p(a, blockIdx.y);
     const int i = (int)a.div_g((uint32_t)r), g = (int)(r - (int64_t)i * a.G);
+    const int steps = dense_key_steps<AXIS, KT>(a, p, r / AXIS * AXIS), pieces = (steps + grid.chunk - 1) / grid.chunk;
+    if (pieces <= 1) return;
     Row acc = Row::zero();
     if (p.seen(a, i) > 0)
-        for (int s = 0; s < grid.splits; ++s) acc.add_part(grid.part + (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r) * D, 1.f, lane);
+        for (int s = 0; s < pieces; ++s) acc.add_part(grid.part + (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r) * D, 1.f, lane);
     acc.scale(a.scale);
     if (a.causal && !acc.finite()) dense_row_dq<T, D>(a, p, i, g, a.nD[blockIdx.y * a.stat_rows + r], lane);
     else acc.store(p.dQ + g * a.q.head + i * a.q.token, lane);
 }
 
-template <class T, int D> __global__ void __launch_bounds__(256) dense_dkv_join_kernel(DenseArgs a, DenseGrid grid) {
+template <class T, int D, int AXIS, int QT> __global__ void __launch_bounds__(256) dense_dkv_join_kernel(DenseArgs a, DenseGrid grid) {
     using Row = LaneRow<T, D>;
     const int lane = threadIdx.x & 63;
     const int64_t j = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (j >= grid.rows) return;
     const DenseGroup p(a, blockIdx.y);
+    int first;
+    const int steps = dense_row_steps<QT>(a, p, (int)(j / AXIS * AXIS), &first), pieces = (steps + grid.chunk - 1) / grid.chunk;
+    if (pieces <= 1) return;
     Row dk = Row::zero(), dv = Row::zero();
     if (j < p.nk) {
-        for (int s = 0; s < grid.splits; ++s) {
+        for (int s = 0; s < pieces; ++s) {
             const float *at = grid.part + (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + j) * (2 * D);
             dk.add_part(at, 1.f, lane);
             dv.add_part(at + D, 1.f, lane);
@@ -255,38 +299,34 @@ template <class T, int D> __global__ void __launch_bounds__(256) dense_dkv_join_
     dv.store(p.dV + j * a.v.token, lane);
 }
 
-// Two workgroups a CU's worth of tiles need no splitting; fewer share out the other axis, at least 4 tiles of 64 each.
-static int bwd_splits(const DensePlan &p, int64_t axis, int64_t other) {
-    const int64_t base = (int64_t)p.desc.batch * p.desc.kv_heads * ((axis + 127) / 128), tiles = (other + 63) / 64;
-    if (base >= 256) return 1;
-    const int64_t want = (512 + base - 1) / base, most = tiles / 4;
-    return (int)(most < 2 ? 1 : want < most ? want : most);
+template <class T, int D, bool NARROW> static hipError_t launch_dq(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
+    constexpr int KT = dense_step(DenseTile<T, D>::ROWB, NARROW);
+    const DenseGrid g = dense_grid(p, p.rows, p.dq, D, part);
+    dense_dq_kernel<T, D, KT, NARROW><<<g.wgs, 256, 0, s>>>(a, g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || g.splits == 1) return e;
+    dense_dq_join_kernel<T, D, dense_tile(NARROW), KT><<<dim3((unsigned)((g.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);
+    return hipGetLastError();
 }
-int dense_dq_splits(const DensePlan &p) { return bwd_splits(p, p.rows, p.desc.Nkv); }
-int dense_dkv_splits(const DensePlan &p) { return bwd_splits(p, p.desc.Nkv, p.rows); }
 
-template <class T, int D> static hipError_t launch_bwd(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
-    constexpr int KT = DenseTile<T, D>::ROWB > 256 ? 32 : 64;
-    const DenseGrid gq = dense_grid(p, p.rows, 128, p.dq_splits, D, part);
-    dense_dq_kernel<T, D, KT><<<gq.wgs, 256, 0, s>>>(a, gq);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && gq.splits > 1) {
-        dense_dq_join_kernel<T, D><<<dim3((unsigned)((gq.rows + 3) / 4), gq.groups), 256, 0, s>>>(a, gq);
-        e = hipGetLastError();
-    }
-    if (e != hipSuccess) return e;
-    const DenseGrid gk = dense_grid(p, p.desc.Nkv, 128, p.dkv_splits, 2 * D, part);
-    dense_dkv_kernel<T, D, KT><<<gk.wgs, 256, 0, s>>>(a, gk);
-    e = hipGetLastError();
-    if (e == hipSuccess && gk.splits > 1) {
-        dense_dkv_join_kernel<T, D><<<dim3((unsigned)((gk.rows + 3) / 4), gk.groups), 256, 0, s>>>(a, gk);
-        e = hipGetLastError();
-    }
-    return e;
+template <class T, int D, bool NARROW> static hipError_t launch_dkv(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
+    constexpr int QT = dense_step(DenseTile<T, D>::ROWB, NARROW);
+    const DenseGrid g = dense_grid(p, p.desc.Nkv, p.dkv, 2 * D, part);
+    dense_dkv_kernel<T, D, QT, NARROW><<<g.wgs, 256, 0, s>>>(a, g);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || g.splits == 1) return e;
+    dense_dkv_join_kernel<T, D, dense_tile(NARROW), QT><<<dim3((unsigned)((g.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);
+    return hipGetLastError();
 }
 
 hipError_t launch_dense_bwd(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
-    return dense_dispatch(p, [&](auto t, auto d) { return launch_bwd<decltype(t), decltype(d)::value>(p, a, part, s); });
+    return dense_dispatch(p, [&](auto t, auto d) {
+        using T = decltype(t);
+        constexpr int D = decltype(d)::value;
+        const hipError_t e = p.dq.narrow ? launch_dq<T, D, true>(p, a, part, s) : launch_dq<T, D, false>(p, a, part, s);
+        if (e != hipSuccess) return e;
+        return p.dkv.narrow ? launch_dkv<T, D, true>(p, a, part, s) : launch_dkv<T, D, false>(p, a, part, s);
+    });
 }
 
 }  // namespace llsa

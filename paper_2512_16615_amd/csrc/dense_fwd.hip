@@ -9,21 +9,25 @@
 
 namespace llsa {
 
-// waves a SIMD that the registers are shared out for
-template <class T, int D, int QB> constexpr int fwd_waves() { return D * (int)sizeof(T) * QB <= 256 ? 2 : 1; }
+// waves a SIMD that the registers are shared out for (a narrow workgroup's rings take all of a CU's LDS at 256 bytes a row)
+template <class T, int D, int QB, bool NARROW> constexpr int fwd_waves() { return D * (int)sizeof(T) * QB <= (NARROW ? 128 : 256) ? 2 : 1; }
 
-template <class T, int D, int QB, int KT>
-__global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
+// NARROW: 32 rows a workgroup, of which each wave has every fourth tile of keys, in stages of its own; the waves' sums are added up at the end.
+template <class T, int D, int QB, int KT, bool NARROW>
+__global__ void __launch_bounds__(256, (fwd_waves<T, D, QB, NARROW>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
     using Tile = DenseTile<T, D>;
-    using Loads = TileLoads<T, D, KT, 4>;
-    constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][TILEB];      // stage; keys, values
+    using Loads = TileLoads<T, D, KT, NARROW ? 1 : 4>;
+    constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32, AXIS = NARROW ? 32 : 128 * QB, WAVES = NARROW ? 4 : 1;
+    constexpr int ST = dense_stages<T, D, NARROW>();                      // (fp32, d = 128, narrow: two stages of each wave would not fit)
+    constexpr int LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * Tile::NB + 2048 : 0;
+    __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];      // wave; stage; keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const DenseWork work = dense_work(grid, a.causal, true);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
-    const int64_t row0 = (int64_t)work.tile * (128 * QB), wrow0 = row0 + wave * (32 * QB);
-    const int end = key_span(a, p, row0, row0 + 128 * QB - 1).some;
+    const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + wave * (32 * QB);
+    const DensePieces piece(grid, work.split, 0, dense_key_steps<AXIS, KT>(a, p, row0));
+    if (piece.none) return;
     const KeySpan mine = key_span(a, p, wrow0, wrow0 + 32 * QB - 1);
 
     // the wave's rows as operands, and what each sees
@@ -54,22 +58,30 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel
         l[c] = 0.f;
     }
 
-    const int tiles = (end + KT - 1) / KT, per = (tiles + grid.splits - 1) / grid.splits;
-    const int t0 = work.split * per, t1 = min(tiles, t0 + per);
+    char *const ring = lds + (NARROW ? wave * (ST * 2 * TILEB) : 0);
+    const unsigned ring0 = lds_address(ring);
+    const int t0 = piece.t0 + (NARROW ? wave : 0);
+    auto stage = [&](int t) { return ST == 1 ? 0 : ((t - t0) / WAVES & 1) * 2 * TILEB; };
     auto fetch = [&](int t) {
         const int k0 = t * KT, left = min(KT, p.nk - k0);
-        const unsigned lds0 = lds_address(&lds[t & 1][0][0]);
-        const unsigned kt = (unsigned)a.k.token, vt = (unsigned)a.v.token;
-        Loads::keys(buffer_of(p.K + k0 * a.k.token, (left - 1) * kt + Tile::ROWB), kt, lds0, wave, lane);
-        Loads::keys(buffer_of(p.V + k0 * a.v.token, (left - 1) * vt + Tile::ROWB), vt, lds0 + TILEB, wave, lane);
+        const unsigned kt = (unsigned)a.k.token, vt = (unsigned)a.v.token, to = ring0 + stage(t);
+        Loads::keys(buffer_of(p.K + k0 * a.k.token, (left - 1) * kt + Tile::ROWB), kt, to, NARROW ? 0 : wave, lane);
+        Loads::keys(buffer_of(p.V + k0 * a.v.token, (left - 1) * vt + Tile::ROWB), vt, to + TILEB, NARROW ? 0 : wave, lane);
     };
-    if (t0 < t1) fetch(t0);
-    for (int t = t0; t < t1; ++t) {
-        vm_wait_barrier<0>();                                // tile t is there, and nobody reads the other stage
-        if (t + 1 < t1) fetch(t + 1);
+    if (ST == 2 && t0 < piece.t1) fetch(t0);
+    loads_done();
+    for (int t = t0; t < piece.t1; t += WAVES) {
+        if (ST == 1) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            fetch(t);
+        }
+        if (NARROW) vm_wait<0>();                            // tile t is there (and nobody else reads the wave's stages),
+        else vm_wait_barrier<0>();                           // for all waves, and nobody reads the other stage
+        if (ST == 2 && t + WAVES < piece.t1) fetch(t + WAVES);
         const int k0 = t * KT;
         if (k0 >= mine.some) continue;
-        const char *kt = &lds[t & 1][0][0], *vt = &lds[t & 1][1][0];
+        const char *kt = ring, *vt = ring + TILEB;
+        const Tile at = tile.at(stage(t));
         f32x16 s[SUBS][QB];
 #pragma unroll
         for (int u = 0; u < SUBS; ++u) {
@@ -79,7 +91,7 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel
                 for (int e = 0; e < 16; ++e) s[u][c][e] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < Tile::KS; ++ks) {
-                const Piece<T> k = tile.row(kt, u, ks);
+                const Piece<T> k = at.row(kt, u, ks);
 #pragma unroll
                 for (int c = 0; c < QB; ++c) s[u][c] = piece_product(k, q[c][ks], s[u][c]);
             }
@@ -126,14 +138,30 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                for (int n = 0; n < Tile::NB; ++n) o[c][n] = tile.col_product(vt, u, n, pr[u], o[c][n]);
+                for (int n = 0; n < Tile::NB; ++n) o[c][n] = at.col_product(vt, u, n, pr[u], o[c][n]);
         }
     }
 
+    if constexpr (NARROW) {                                  // each wave's exponentials are relative to its own reference
+        __syncthreads();
+        float *ml = reinterpret_cast<float *>(lds + 12288 * Tile::NB);
+        ml[wave * 64 + lane] = m[0];
+        ml[256 + wave * 64 + lane] = l[0];
+        __syncthreads();
+        float top = m[0], sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * 64 + lane]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) sum = fmaf(ml[256 + w * 64 + lane], __builtin_amdgcn_exp2f(ml[w * 64 + lane] - top), sum);
+        add_waves(o[0], __builtin_amdgcn_exp2f(m[0] - top), lds, wave, lane);
+        if (wave > 0) return;
+        m[0] = top;
+        l[0] = sum;
+    }
 #pragma unroll
     for (int c = 0; c < QB; ++c) {
         const float sum = half_sum(l[c]);
-        if (grid.splits > 1) {
+        if (!piece.alone) {
             const int64_t at = ((int64_t)work.split * grid.groups + work.group) * grid.rows + wrow0 + 32 * c + col;
             if (qi[c] >= 0) {
                 store_partial<D>(grid.part + at * D, o[c], h);
@@ -164,8 +192,8 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel
     }
 }
 
-// The splits' partial sums of a row, one wave a row: the exponentials of split i are relative to its own reference.
-template <class T, int D> __global__ void __launch_bounds__(256) dense_join_kernel(DenseArgs a, DenseGrid grid) {
+// The pieces' partial sums of a row, one wave a row: the exponentials of each are relative to its own reference.
+template <class T, int D, int AXIS, int KT> __global__ void __launch_bounds__(256) dense_join_kernel(DenseArgs a, DenseGrid grid) {
     using Row = LaneRow<T, D>;
     const int lane = threadIdx.x & 63;
     const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -173,11 +201,13 @@ template <class T, int D> __global__ void __launch_bounds__(256) dense_join_kern
     const DenseGroup p(a, blockIdx.y);
     const int i = (int)a.div_g((uint32_t)r), g = (int)(r - (int64_t)i * a.G);
     char *dst = p.out + g * a.o.head + i * a.o.token;
+    const int steps = dense_key_steps<AXIS, KT>(a, p, r / AXIS * AXIS), pieces = (steps + grid.chunk - 1) / grid.chunk;
+    if (pieces <= 1) return;                                 // the forward launch's result already
     const bool any = p.seen(a, i) > 0;
     float m = -3e38f, l = 0.f;
-    for (int s = 0; s < grid.splits; ++s) m = fmaxf(m, grid.stat[2 * (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r)]);
+    for (int s = 0; s < pieces; ++s) m = fmaxf(m, grid.stat[2 * (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r)]);
     Row acc = Row::zero();
-    for (int s = 0; s < grid.splits; ++s) {
+    for (int s = 0; s < pieces; ++s) {
         const int64_t at = ((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r;
         const float2 st = *reinterpret_cast<const float2 *>(grid.stat + 2 * at);
         const float f = __builtin_amdgcn_exp2f(st.x - m);
@@ -194,26 +224,20 @@ template <class T, int D> __global__ void __launch_bounds__(256) dense_join_kern
     if (lane == 0) p.LSE[(int64_t)g * a.Nq + i] = any ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
-// Two workgroups a CU's worth of tiles need no splitting; fewer rows share out the keys, at least 4 tiles of 64 each.
-int dense_fwd_splits(const DensePlan &p) {
-    const int64_t base = (int64_t)p.desc.batch * p.desc.kv_heads * ((p.rows + 127) / 128), tiles = (p.desc.Nkv + 63) / 64;
-    if (base >= 256) return 1;
-    const int64_t want = (512 + base - 1) / base, most = tiles / 4;
-    return (int)(most < 2 ? 1 : want < most ? want : most);
-}
-
-template <class T, int D> static hipError_t launch_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
-    constexpr int KT = DenseTile<T, D>::ROWB > 256 ? 32 : 64;
-    DenseGrid g = dense_grid(p, p.rows, 128, p.fwd_splits, D, ws);
-    dense_fwd_kernel<T, D, 1, KT><<<g.wgs, 256, 0, s>>>(a, g);
-    hipError_t e = hipGetLastError();
+template <class T, int D, bool NARROW> static hipError_t launch_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
+    constexpr int KT = dense_step(DenseTile<T, D>::ROWB, NARROW);
+    const DenseGrid g = dense_grid(p, p.rows, p.fwd, D, ws);
+    dense_fwd_kernel<T, D, 1, KT, NARROW><<<g.wgs, 256, 0, s>>>(a, g);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1) return e;
-    dense_join_kernel<T, D><<<dim3((unsigned)((p.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);
+    dense_join_kernel<T, D, dense_tile(NARROW), KT><<<dim3((unsigned)((p.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);
     return hipGetLastError();
 }
 
 hipError_t launch_dense_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
-    return dense_dispatch(p, [&](auto t, auto d) { return launch_fwd<decltype(t), decltype(d)::value>(p, a, ws, s); });
+    return dense_dispatch(p, [&](auto t, auto d) {
+        return p.fwd.narrow ? launch_fwd<decltype(t), decltype(d)::value, true>(p, a, ws, s) : launch_fwd<decltype(t), decltype(d)::value, false>(p, a, ws, s);
+    });
 }
 
 }  // namespace llsa

@@ -108,6 +108,26 @@ __device__ __forceinline__ KeySpan key_span(const DenseArgs &a, const DenseGroup
     return {p.seen(a, q0), p.seen(a, q1)};
 }
 
+// The tiles of the other axis that a workgroup has: piece `split` of its tile's `tiles`, which begin at `first`.  One piece at least: `alone`, its sums are the result.
+struct DensePieces {
+    int t0, t1;
+    bool alone, none;
+    __device__ __forceinline__ DensePieces(const DenseGrid &g, int split, int first, int tiles) {
+        t0 = first + split * g.chunk;
+        t1 = min(first + tiles, t0 + g.chunk);
+        alone = tiles <= g.chunk;
+        none = split > 0 && t0 >= t1;
+    }
+};
+// .. of a tile of rows, and of a tile of keys
+template <int AXIS, int STEP> __device__ __forceinline__ int dense_key_steps(const DenseArgs &a, const DenseGroup &p, int64_t row0) {
+    return (key_span(a, p, row0, row0 + AXIS - 1).some + STEP - 1) / STEP;
+}
+template <int STEP> __device__ __forceinline__ int dense_row_steps(const DenseArgs &a, const DenseGroup &p, int key0, int *first) {
+    *first = p.first_query(a, key0) * a.G / STEP;
+    return max(0, (p.nq * a.G + STEP - 1) / STEP - *first);
+}
+
 // Which rows and keys a workgroup has.  Causal: the tiles with the most work first (the last
 // rows, the first keys), of all groups in turn; otherwise the tiles of a group next to each
 // other and the groups in stretches, so that the workgroups of one XCD share their keys.

@@ -95,6 +95,15 @@ template <class T, int D> struct DenseTile {
             lane_col = 4 * h * ROWB + (((c >> 2) ^ h) << 4) + ((c & 3) << 2);
         }
     }
+    // The same for a stage's tiles, `offset` bytes on (a multiple of 1024).  Opaque: the compiler would keep each of the sixteen places that are an exclusive
+    // or away from these in a register of its own over the whole loop, and spill others.
+    __device__ __forceinline__ DenseTile at(int offset) const {
+        DenseTile t = *this;
+        t.lane_row += offset;
+        t.lane_col += offset;
+        asm volatile("" : "+v"(t.lane_row), "+v"(t.lane_col));
+        return t;
+    }
     // piece ks of row 32 sub + i
     __device__ __forceinline__ Piece<T> row(const char *tile, int sub, int ks) const {
         return {*reinterpret_cast<const u32x4 *>(tile + (lane_row ^ (32 * ks)) + sub * 32 * ROWB)};
@@ -118,6 +127,9 @@ template <class T, int D> struct DenseTile {
         return acc;
     }
 };
+
+// Stages of a ring of two tensors' tiles: two, but where four waves of a narrow workgroup have rings of 512-byte rows
+template <class T, int D, bool NARROW> constexpr int dense_stages() { return NARROW && DenseTile<T, D>::ROWB > 256 ? 1 : 2; }
 
 // Memory straight into LDS through a buffer descriptor: lane l fetches 16 bytes at its own offset, to 16 l of the 1024 bytes at `lds`; what lies
 // outside the descriptor's bytes arrives as zeros.  The asm begins with the wait states that a vector memory instruction needs behind a
@@ -148,6 +160,10 @@ __device__ __forceinline__ void buffer_to_lds_dword(u32x4 buf, unsigned v, unsig
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(v), "s"(buf), "s"(lds) : "memory", "m0");
 }
 #pragma clang diagnostic pop
+
+// Every load that the compiler knows of is done.  In front of a loop that waits for its ring by itself: the compiler would wait inside it, in each
+// round, for what the first one uses, and so for the ring's newest tile (causal, 3 x 16 heads x 1999 tokens, d = 128: forward 59 -> 40 us).
+__device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 // A wave's share of a tile of ROWS rows: loads first, first + 1, .. of it (1024 bytes each).
 template <class T, int D, int ROWS, int WAVES> struct TileLoads {
@@ -190,6 +206,33 @@ template <class T, int D, int ROWS, int WAVES> struct TileLoads {
         }
     }
 };
+
+// The sums of a workgroup's four waves over the same rows, in wave 0 (f: what the lane's own are multiplied by; the waves' in order).  A lane has the
+// same rows and channels in each wave, so registers go through LDS as they are.  lds: 12 KB a block, free of everything else.
+template <int NB> __device__ __forceinline__ void add_waves(f32x16 (&acc)[NB], float f, char *lds, int wave, int lane) {
+    f32x4 *buf = reinterpret_cast<f32x4 *>(lds);
+    if (wave > 0) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                buf[(((wave - 1) * NB + n) * 4 + k) * 64 + lane] = f32x4{acc[n][4 * k] * f, acc[n][4 * k + 1] * f, acc[n][4 * k + 2] * f, acc[n][4 * k + 3] * f};
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float x = acc[n][4 * k + e] * f;
+#pragma unroll
+                    for (int w = 0; w < 3; ++w) x += buf[((w * NB + n) * 4 + k) * 64 + lane][e];
+                    acc[n][4 * k + e] = x;
+                }
+    }
+}
 
 // 32 rows' results (32-channel blocks, column = row of the tensor) to memory: scaled, rounded once; 16 bytes a lane.
 template <class T, int D> __device__ __forceinline__ void store_rows(char *row, const f32x16 (&acc)[DenseTile<T, D>::NB], float f, int h, bool write) {
