@@ -8,12 +8,13 @@
 
 namespace llsa {
 
-// waves a SIMD that the registers are shared out for (a narrow workgroup's rings take all of a CU's LDS at 256 bytes a row)
-template <class T, int D, bool NARROW> constexpr int bwd_waves() { return D * (int)sizeof(T) <= (NARROW ? 128 : 256) ? 2 : 1; }
+// waves a SIMD that the registers are shared out for (the key-major sums of a narrow workgroup take more than half of a CU's LDS at d = 128)
+template <class T, int D> constexpr int dq_waves() { return D * (int)sizeof(T) <= 256 ? 2 : 1; }
+template <class T, int D, bool NARROW> constexpr int dkv_waves() { return D * (int)sizeof(T) <= 256 && !(NARROW && D == 128) ? 2 : 1; }
 
 // NARROW: 32 rows a workgroup, of which each wave has every fourth tile of keys, in stages of its own; the waves' sums are added up at the end.
 template <class T, int D, int KT, bool NARROW>
-__global__ void __launch_bounds__(256, (bwd_waves<T, D, NARROW>())) dense_dq_kernel(DenseArgs a, DenseGrid grid) {
+__global__ void __launch_bounds__(256, (dq_waves<T, D>())) dense_dq_kernel(DenseArgs a, DenseGrid grid) {
     using Tile = DenseTile<T, D>;
     using Loads = TileLoads<T, D, KT, NARROW ? 1 : 4>;
     constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1;
@@ -24,24 +25,26 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D, NARROW>())) dense_dq_ker
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
     const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + wave * 32, r = wrow0 + col;
+    // All rows are read, those behind the length too, so that they are on their way before the lengths are there: what such a row holds stays in its lane.
+    const bool in = r < grid.rows;
+    const int qi = (int)a.div_g((uint32_t)(in ? r : 0)), qg = (int)((in ? r : 0) - (int64_t)qi * a.G);
+    const int64_t at_q = qg * a.q.head + (int64_t)qi * a.q.token, at_o = qg * a.o.head + (int64_t)qi * a.o.token;
+    Piece<T> q[Tile::KS], g[Tile::KS], o[Tile::KS];
+#pragma unroll
+    for (int ks = 0; ks < Tile::KS; ++ks) {
+        q[ks].w = *reinterpret_cast<const u32x4 *>(p.Q + at_q + 16 * h + 32 * ks);
+        g[ks].w = *reinterpret_cast<const u32x4 *>(p.dO + at_o + 16 * h + 32 * ks);
+        o[ks].w = *reinterpret_cast<const u32x4 *>(p.O + at_o + 16 * h + 32 * ks);
+    }
+    const float lse = p.LSE[(int64_t)qg * a.Nq + qi];
     const DensePieces piece(grid, work.split, 0, dense_key_steps<AXIS, KT>(a, p, row0));
     if (piece.none) return;
     const KeySpan mine = key_span(a, p, wrow0, wrow0 + 31);
-
-    const bool in = r < grid.rows;
-    const int qi = (int)a.div_g((uint32_t)(in ? r : 0)), qg = (int)((in ? r : 0) - (int64_t)qi * a.G), seen = in ? p.seen(a, qi) : 0;
-    const int64_t at_q = qg * a.q.head + (int64_t)qi * a.q.token, at_o = qg * a.o.head + (int64_t)qi * a.o.token;
-    Piece<T> q[Tile::KS], g[Tile::KS];
+    const int seen = in ? p.seen(a, qi) : 0;
     float delta = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < Tile::KS; ++ks) {
-        const u32x4 zero = {0, 0, 0, 0};
-        q[ks].w = seen > 0 ? *reinterpret_cast<const u32x4 *>(p.Q + at_q + 16 * h + 32 * ks) : zero;
-        g[ks].w = seen > 0 ? *reinterpret_cast<const u32x4 *>(p.dO + at_o + 16 * h + 32 * ks) : zero;
-        const Piece<T> o = {seen > 0 ? *reinterpret_cast<const u32x4 *>(p.O + at_o + 16 * h + 32 * ks) : zero};
-        delta = piece_dot(g[ks], o, delta);
-    }
-    const float nD = -half_sum(delta), nlse = seen > 0 ? -p.LSE[(int64_t)qg * a.Nq + qi] / a.scale : -INFINITY;
+    for (int ks = 0; ks < Tile::KS; ++ks) delta = piece_dot(g[ks], o[ks], delta);
+    const float nD = seen > 0 ? -half_sum(delta) : 0.f, nlse = seen > 0 ? -lse / a.scale : -INFINITY;
     if (work.split == 0 && h == 0 && (!NARROW || wave == 0)) {                         // also for the rows that the last tile has too many
         a.nD[work.group * a.stat_rows + r] = nD;
         a.nlse[work.group * a.stat_rows + r] = nlse;
@@ -126,7 +129,7 @@ __global__ void __launch_bounds__(256, (bwd_waves<T, D, NARROW>())) dense_dq_ker
 // A wave has 32 keys, theirs and their values' channels in registers, and walks over the rows (of every head that shares them) in tiles of QT.
 // NARROW: 32 keys a workgroup, for which each wave has every fourth tile of rows, in stages of its own.
 template <class T, int D, int QT, bool NARROW>
-__global__ void __launch_bounds__(256, (bwd_waves<T, D, NARROW>())) dense_dkv_kernel(DenseArgs a, DenseGrid grid) {
+__global__ void __launch_bounds__(256, (dkv_waves<T, D, NARROW>())) dense_dkv_kernel(DenseArgs a, DenseGrid grid) {
     using Tile = DenseTile<T, D>;
     using Loads = TileLoads<T, D, QT, NARROW ? 1 : 4>;
     constexpr int TILEB = QT * Tile::ROWB, SUBS = QT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1;
@@ -266,8 +269,9 @@ template <class T, int D, int AXIS, int KT> __global__ void __launch_bounds__(25
     const int steps = dense_key_steps<AXIS, KT>(a, p, r / AXIS * AXIS), pieces = (steps + grid.chunk - 1) / grid.chunk;
     if (pieces <= 1) return;
     Row acc = Row::zero();
+    const int64_t step = (int64_t)grid.groups * grid.rows * D;
     if (p.seen(a, i) > 0)
-        for (int s = 0; s < pieces; ++s) acc.add_part(grid.part + (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r) * D, 1.f, lane);
+        for (int s = 0; s < pieces; s += 64) acc.add_parts(grid.part + ((int64_t)blockIdx.y * grid.rows + r) * D + s * step, step, min(64, pieces - s), 1.f, lane);
     acc.scale(a.scale);
     if (a.causal && !acc.finite()) dense_row_dq<T, D>(a, p, i, g, a.nD[blockIdx.y * a.stat_rows + r], lane);
     else acc.store(p.dQ + g * a.q.head + i * a.q.token, lane);
@@ -284,10 +288,11 @@ template <class T, int D, int AXIS, int QT> __global__ void __launch_bounds__(25
     if (pieces <= 1) return;
     Row dk = Row::zero(), dv = Row::zero();
     if (j < p.nk) {
-        for (int s = 0; s < pieces; ++s) {
-            const float *at = grid.part + (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + j) * (2 * D);
-            dk.add_part(at, 1.f, lane);
-            dv.add_part(at + D, 1.f, lane);
+        const int64_t step = (int64_t)grid.groups * grid.rows * (2 * D);
+        const float *at = grid.part + ((int64_t)blockIdx.y * grid.rows + j) * (2 * D);
+        for (int s = 0; s < pieces; s += 64) {
+            dk.add_parts(at + s * step, step, min(64, pieces - s), 1.f, lane);
+            dv.add_parts(at + D + s * step, step, min(64, pieces - s), 1.f, lane);
         }
         dk.scale(a.scale);
         if (a.causal && !(dk.finite() && dv.finite())) {

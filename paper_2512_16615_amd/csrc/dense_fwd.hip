@@ -9,16 +9,16 @@
 
 namespace llsa {
 
-// waves a SIMD that the registers are shared out for (a narrow workgroup's rings take all of a CU's LDS at 256 bytes a row)
-template <class T, int D, int QB, bool NARROW> constexpr int fwd_waves() { return D * (int)sizeof(T) * QB <= (NARROW ? 128 : 256) ? 2 : 1; }
+// waves a SIMD that the registers are shared out for
+template <class T, int D, int QB> constexpr int fwd_waves() { return D * (int)sizeof(T) * QB <= 256 ? 2 : 1; }
 
 // NARROW: 32 rows a workgroup, of which each wave has every fourth tile of keys, in stages of its own; the waves' sums are added up at the end.
 template <class T, int D, int QB, int KT, bool NARROW>
-__global__ void __launch_bounds__(256, (fwd_waves<T, D, QB, NARROW>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
+__global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
     using Tile = DenseTile<T, D>;
     using Loads = TileLoads<T, D, KT, NARROW ? 1 : 4>;
     constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32, AXIS = NARROW ? 32 : 128 * QB, WAVES = NARROW ? 4 : 1;
-    constexpr int ST = dense_stages<T, D, NARROW>();                      // (fp32, d = 128, narrow: two stages of each wave would not fit)
+    constexpr int ST = dense_stages<T, D, NARROW>();
     constexpr int LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * Tile::NB + 2048 : 0;
     __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];      // wave; stage; keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
@@ -26,11 +26,8 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, QB, NARROW>())) dense_fw
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
     const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + wave * (32 * QB);
-    const DensePieces piece(grid, work.split, 0, dense_key_steps<AXIS, KT>(a, p, row0));
-    if (piece.none) return;
-    const KeySpan mine = key_span(a, p, wrow0, wrow0 + 32 * QB - 1);
-
-    // the wave's rows as operands, and what each sees
+    // The wave's rows as operands, and what each sees.  All rows are read, those behind the length too, so that they are on their way before the
+    // lengths are there: whatever such a row holds stays in its own lane.
     Piece<T> q[QB][Tile::KS];
     int seen[QB], qi[QB], qg[QB];
 #pragma unroll
@@ -39,12 +36,16 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, QB, NARROW>())) dense_fw
         const bool in = r < grid.rows;
         qi[c] = (int)a.div_g((uint32_t)(in ? r : 0));
         qg[c] = (int)((in ? r : 0) - (int64_t)qi[c] * a.G);
-        seen[c] = in ? p.seen(a, qi[c]) : 0;
-        if (!in) qi[c] = -1;
-        const char *src = p.Q + qg[c] * a.q.head + (int64_t)max(qi[c], 0) * a.q.token + 16 * h;
+        const char *src = p.Q + qg[c] * a.q.head + qi[c] * a.q.token + 16 * h;
 #pragma unroll
-        for (int ks = 0; ks < Tile::KS; ++ks) q[c][ks].w = seen[c] > 0 ? *reinterpret_cast<const u32x4 *>(src + 32 * ks) : u32x4{0, 0, 0, 0};
+        for (int ks = 0; ks < Tile::KS; ++ks) q[c][ks].w = *reinterpret_cast<const u32x4 *>(src + 32 * ks);
+        if (!in) qi[c] = -1;
     }
+    const DensePieces piece(grid, work.split, 0, dense_key_steps<AXIS, KT>(a, p, row0));
+    if (piece.none) return;
+    const KeySpan mine = key_span(a, p, wrow0, wrow0 + 32 * QB - 1);
+#pragma unroll
+    for (int c = 0; c < QB; ++c) seen[c] = qi[c] >= 0 ? p.seen(a, qi[c]) : 0;
 
     f32x16 o[QB][Tile::NB];
     float m[QB], l[QB];                                      // the reference that the exponentials are relative to (log2), their sum in this lane
@@ -204,15 +205,17 @@ template <class T, int D, int AXIS, int KT> __global__ void __launch_bounds__(25
     const int steps = dense_key_steps<AXIS, KT>(a, p, r / AXIS * AXIS), pieces = (steps + grid.chunk - 1) / grid.chunk;
     if (pieces <= 1) return;                                 // the forward launch's result already
     const bool any = p.seen(a, i) > 0;
+    const int64_t at = (int64_t)blockIdx.y * grid.rows + r, step = (int64_t)grid.groups * grid.rows;     // piece 0's sums; from piece to piece
     float m = -3e38f, l = 0.f;
-    for (int s = 0; s < pieces; ++s) m = fmaxf(m, grid.stat[2 * (((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r)]);
+    for (int s = lane; s < pieces; s += 64) m = fmaxf(m, grid.stat[2 * (at + s * step)]);
+    m = wave_max(m);
     Row acc = Row::zero();
-    for (int s = 0; s < pieces; ++s) {
-        const int64_t at = ((int64_t)s * grid.groups + blockIdx.y) * grid.rows + r;
-        const float2 st = *reinterpret_cast<const float2 *>(grid.stat + 2 * at);
-        const float f = __builtin_amdgcn_exp2f(st.x - m);
-        l = fmaf(f, st.y, l);
-        acc.add_part(grid.part + at * D, f, lane);
+    for (int s0 = 0; s0 < pieces; s0 += 64) {
+        const int s = s0 + lane;
+        const float2 st = s < pieces ? *reinterpret_cast<const float2 *>(grid.stat + 2 * (at + s * step)) : make_float2(-3e38f, 0.f);
+        const float f = s < pieces ? __builtin_amdgcn_exp2f(st.x - m) : 0.f;
+        l += wave_sum(f * st.y);
+        acc.add_parts(grid.part + (at + s0 * step) * D, step * D, min(64, pieces - s0), f, lane);
     }
     if (any) acc.scale(1.f / l);
     else acc = Row::zero();

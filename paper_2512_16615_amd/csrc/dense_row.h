@@ -7,6 +7,12 @@
 
 namespace llsa {
 
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+    return x;
+}
+
 template <class T> __device__ __forceinline__ float dense_ld(const char *row, int c);
 template <> __device__ __forceinline__ float dense_ld<float>(const char *row, int c) { return reinterpret_cast<const float *>(row)[c]; }
 template <> __device__ __forceinline__ float dense_ld<__bf16>(const char *row, int c) { return (float)reinterpret_cast<const __bf16 *>(row)[c]; }
@@ -47,11 +53,22 @@ template <class T, int D> struct LaneRow {
 #pragma unroll
         for (int k = 0; k < n; ++k) x[k] = fmaf(f, o.x[k], x[k]);
     }
-    // += f times d partial sums
-    __device__ __forceinline__ void add_part(const float *part, float f, int lane) {
+    // += f[s] times d partial sums, s = 0 .. n - 1 in order, `stride` floats apart; f[s] is lane s's.  Eight of them on their way at once.
+    __device__ __forceinline__ void add_parts(const float *part, int64_t stride, int n, float f, int lane) {
+        for (int s = 0; s < n; s += 8) {
+            float v[8][LaneRow::n];
 #pragma unroll
-        for (int k = 0; k < n; ++k)
-            if (lane + 64 * k < D) x[k] = fmaf(f, part[lane + 64 * k], x[k]);
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int k = 0; k < LaneRow::n; ++k) v[i][k] = lane + 64 * k < D ? part[min(s + i, n - 1) * stride + lane + 64 * k] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (s + i >= n) break;
+                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), s + i));
+#pragma unroll
+                for (int k = 0; k < LaneRow::n; ++k) x[k] = fmaf(w, v[i][k], x[k]);
+            }
+        }
     }
     // in every lane of the wave
     __device__ __forceinline__ bool finite() const {

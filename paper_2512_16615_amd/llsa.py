@@ -189,6 +189,7 @@ class Plan:
         self._shape = torch.Size((batch, heads, N, d))
         self._workspace_bytes = tuple(lib.llsa_plan_workspace_bytes(self._h, i) for i in (0, 1))
         self._indices_bytes = lib.llsa_plan_indices_bytes(self._h)
+        self._glue_bytes = lib.llsa_qknorm_rope_backward_bytes(self._h)
         self.levels = [self.level_info(l) for l in range(L)]
 
     def __del__(self):
@@ -229,7 +230,7 @@ class Plan:
 
     def alloc_glue_workspace(self, device="cuda") -> torch.Tensor:
         """Workspace of ``qknorm_rope_backward``."""
-        return torch.empty(load().llsa_qknorm_rope_backward_bytes(self._h), dtype=torch.uint8, device=device)
+        return torch.empty(self._glue_bytes, dtype=torch.uint8, device=device)
 
     def level_indices(self, indices: torch.Tensor, l: int) -> torch.Tensor:
         """View of I^(l) inside ``indices``: ``[batch, heads, rows, K_l]``."""
@@ -291,27 +292,28 @@ def qknorm_rope_pool(p: Plan, Qpre, Kpre, V, gamma_q, gamma_k, cos_table, sin_ta
     return Qout, Kout, workspace
 
 
-def _chk_here(t: torch.Tensor, name: str):
-    """The kernels run on the current device's current stream."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise LlsaError(f"{name}: expected a tensor on the current device, got one on {t.device}")
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
-def _chk_vec(t: torch.Tensor, name: str, dtype, shape, last_only=False):
-    """A tensor of exactly this type and shape; contiguous, or with contiguous rows."""
-    _chk_here(t, name)
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise LlsaError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    if not (t.is_contiguous() or last_only and t.stride(-1) == 1):
-        raise LlsaError(f"{name}: expected a contiguous tensor, got strides {t.stride()}")
+def _device() -> int:
+    """The current device, on whose current stream the kernels run (torch.cuda.current_device() takes three times as long)."""
+    try:
+        return torch.cuda.current_device() if _raw_device is None else _raw_device()
+    except RuntimeError as e:
+        raise LlsaError(f"no current device: {e}") from None
 
 
-def _chk_ws(t: torch.Tensor | None, name: str, nbytes: int):
-    if t is None:
+def _chk_vec(t: torch.Tensor, name: str, dtype, shape, dev: int, rows_only=False):
+    """A tensor of exactly this type and shape on device ``dev``; contiguous, or with contiguous rows."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and (t.is_contiguous() or rows_only and t.stride(-1) == 1):
         return
-    _chk_here(t, name)
-    if t.numel() * t.element_size() < nbytes or not t.is_contiguous():
-        raise LlsaError(f"{name}: {nbytes} contiguous bytes are needed")
+    raise LlsaError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev}, got {t.dtype} {tuple(t.shape)} "
+                    f"with strides {t.stride()} on {t.device}")
+
+
+def _chk_ws(t: torch.Tensor | None, name: str, nbytes: int, dev: int):
+    if t is not None and (t.get_device() != dev or not t.is_contiguous() or t.numel() * t.element_size() < nbytes):
+        raise LlsaError(f"{name}: {nbytes} contiguous bytes on device {dev} are needed")
 
 
 def qknorm_rope_backward(p: Plan, Qpre, Kpre, gamma_q, gamma_k, cos_table, sin_table, dQ, dK, eps=1e-6, dQpre=None, dKpre=None,
@@ -320,18 +322,20 @@ def qknorm_rope_backward(p: Plan, Qpre, Kpre, gamma_q, gamma_k, cos_table, sin_t
     ``qknorm_rope_pool`` made (as ``backward`` returns them).  ``dQpre`` may be ``dQ``, ``dKpre`` ``dK``."""
     dQpre = torch.empty_like(Qpre) if dQpre is None else dQpre
     dKpre = torch.empty_like(Kpre) if dKpre is None else dKpre
+    dev, dt, shape, f32 = _device(), p.torch_dtype, p._shape, torch.float32
     for t, n in ((Qpre, "Qpre"), (Kpre, "Kpre"), (dQ, "dQ"), (dK, "dK"), (dQpre, "dQpre"), (dKpre, "dKpre")):
-        _chk_here(t, n)
-        _chk_tensor(p, t, n)
+        _chk_vec(t, n, dt, shape, dev)
     dgamma_q = torch.empty(p.d, dtype=torch.float32, device=Qpre.device) if dgamma_q is None else dgamma_q
     dgamma_k = torch.empty(p.d, dtype=torch.float32, device=Qpre.device) if dgamma_k is None else dgamma_k
-    for t, shape, n in ((gamma_q, (p.d,), "gamma_q"), (gamma_k, (p.d,), "gamma_k"), (dgamma_q, (p.d,), "dgamma_q"), (dgamma_k, (p.d,), "dgamma_k"),
-                        (cos_table, (p.N, p.d // 2), "cos_table"), (sin_table, (p.N, p.d // 2), "sin_table")):
-        _chk_vec(t, n, torch.float32, shape)
+    vec, table = (p.d,), (p.N, p.d // 2)
+    for t, n in ((gamma_q, "gamma_q"), (gamma_k, "gamma_k"), (dgamma_q, "dgamma_q"), (dgamma_k, "dgamma_k")):
+        _chk_vec(t, n, f32, vec, dev)
+    _chk_vec(cos_table, "cos_table", f32, table, dev)
+    _chk_vec(sin_table, "sin_table", f32, table, dev)
     workspace = p.alloc_glue_workspace(Qpre.device) if workspace is None else workspace
-    _chk_ws(workspace, "workspace", load().llsa_qknorm_rope_backward_bytes(p._h))
+    _chk_ws(workspace, "workspace", p._glue_bytes, dev)
     _check(load().llsa_qknorm_rope_backward(p._h, _ptr(Qpre), _ptr(Kpre), _ptr(gamma_q), _ptr(gamma_k), _ptr(cos_table), _ptr(sin_table),
-                                            ctypes.c_float(eps), _ptr(dQ), _ptr(dK), _ptr(dQpre), _ptr(dKpre), _ptr(dgamma_q),
+                                            eps, _ptr(dQ), _ptr(dK), _ptr(dQpre), _ptr(dKpre), _ptr(dgamma_q),
                                             _ptr(dgamma_k), _ptr(workspace), _stream()), "llsa_qknorm_rope_backward")
     return dQpre, dKpre, dgamma_q, dgamma_k
 
@@ -456,7 +460,7 @@ class DensePlan:
         _check(st, "llsa_dense_plan")
         self.batch, self.heads, self.kv_heads, self.Nq, self.Nkv, self.d = batch, heads, kv_heads, Nq, Nkv, d
         self.torch_dtype = torch.float32 if dtype == F32 else torch.bfloat16
-        self._q, self._kv = torch.Size((batch, heads, Nq, d)), torch.Size((batch, kv_heads, Nkv, d))
+        self._q, self._kv, self._rows = torch.Size((batch, heads, Nq, d)), torch.Size((batch, kv_heads, Nkv, d)), torch.Size((batch, heads, Nq))
         self._strides = {}
         for name, st, size in zip("qkvo", strides, (self._q, self._kv, self._kv, self._q)):
             if not any(st):
@@ -484,50 +488,50 @@ class DensePlan:
             raise LlsaError(f"{which}: rows of a tensor to be written would overlap")
         return torch.empty_strided(size, st, dtype=self.torch_dtype, device=device)
 
-    def _check_tensor(self, t: torch.Tensor, name: str, which: str):
-        size = self._q if which in "qo" else self._kv
-        if t.dtype != self.torch_dtype or t.shape != size or any(n > 1 and a != b for n, a, b in zip(size, t.stride(), self._strides[which])):
-            raise LlsaError(f"{name}: expected {self.torch_dtype} {tuple(size)} with strides {self._strides[which]}, got {t.dtype} "
-                            f"{tuple(t.shape)} with strides {t.stride()}")
-        _chk_here(t, name)
-
-    def _check_lens(self, q_lens, kv_lens):
-        for t, n in ((q_lens, "q_lens"), (kv_lens, "kv_lens")):
+    def _check(self, tensors, vectors, dev: int):
+        """Tensors of the plan's layout ("q", "k", "v" or "o") and contiguous ones of a type and shape, all on device ``dev``; None: not given."""
+        dt = self.torch_dtype
+        for t, name, which in tensors:
+            size, st = self._kv if which in "kv" else self._q, self._strides[which]
+            if t.dtype is dt and t.shape == size and t.get_device() == dev and \
+                    (t.stride() == st or all(n == 1 or a == b for n, a, b in zip(size, t.stride(), st))):
+                continue
+            raise LlsaError(f"{name}: expected {dt} {tuple(size)} with strides {st} on device {dev}, got {t.dtype} {tuple(t.shape)} "
+                            f"with strides {t.stride()} on {t.device}")
+        for t, name, dtype, shape in vectors:
             if t is not None:
-                _chk_vec(t, n, torch.int32, (self.batch,))
+                _chk_vec(t, name, dtype, shape, dev)
 
 
 def dense_forward(p: DensePlan, Q, K, V, q_lens=None, kv_lens=None, O=None, LSE=None, workspace=None):
     """``llsa_dense_forward``: returns ``(O, LSE)``.  ``q_lens``, ``kv_lens``: ``[batch]`` int32 on the device."""
-    p._check_tensor(Q, "Q", "q")
-    p._check_tensor(K, "K", "k")
-    p._check_tensor(V, "V", "v")
-    p._check_lens(q_lens, kv_lens)
+    dev, lens = _device(), (p.batch,)
     O = p.empty("o", Q.device) if O is None else O
-    p._check_tensor(O, "O", "o")
-    LSE = torch.empty(p.batch, p.heads, p.Nq, dtype=torch.float32, device=Q.device) if LSE is None else LSE
-    _chk_vec(LSE, "LSE", torch.float32, (p.batch, p.heads, p.Nq))
+    LSE = torch.empty(p._rows, dtype=torch.float32, device=Q.device) if LSE is None else LSE
+    p._check(((Q, "Q", "q"), (K, "K", "k"), (V, "V", "v"), (O, "O", "o")),
+             ((LSE, "LSE", torch.float32, p._rows), (q_lens, "q_lens", torch.int32, lens), (kv_lens, "kv_lens", torch.int32, lens)), dev)
     need = p._workspace_bytes[0]
-    workspace = p.alloc_workspace(False, Q.device) if workspace is None and need else workspace
-    _chk_ws(workspace, "workspace", need)
-    _check(load().llsa_dense_forward(p._h, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_lens), _ptr(kv_lens), _ptr(O), _ptr(LSE), _ptr(workspace),
-                                     _stream()), "llsa_dense_forward")
+    if need:
+        workspace = p.alloc_workspace(False, Q.device) if workspace is None else workspace
+        _chk_ws(workspace, "workspace", need, dev)
+    _check(load().llsa_dense_forward(p._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _ptr(q_lens), _ptr(kv_lens), O.data_ptr(), LSE.data_ptr(),
+                                     workspace.data_ptr() if need else None, _stream()), "llsa_dense_forward")
     return O, LSE
 
 
 def dense_backward(p: DensePlan, Q, K, V, O, LSE, dO, q_lens=None, kv_lens=None, dQ=None, dK=None, dV=None, workspace=None):
     """``llsa_dense_backward``: returns ``(dQ, dK, dV)``, with the strides of Q, K and V."""
+    dev, lens = _device(), (p.batch,)
     dQ = p.empty("q", Q.device) if dQ is None else dQ
     dK = p.empty("k", Q.device) if dK is None else dK
     dV = p.empty("v", Q.device) if dV is None else dV
-    for t, n, which in ((Q, "Q", "q"), (K, "K", "k"), (V, "V", "v"), (O, "O", "o"), (dO, "dO", "o"), (dQ, "dQ", "q"), (dK, "dK", "k"), (dV, "dV", "v")):
-        p._check_tensor(t, n, which)
-    p._check_lens(q_lens, kv_lens)
-    _chk_vec(LSE, "LSE", torch.float32, (p.batch, p.heads, p.Nq))
+    p._check(((Q, "Q", "q"), (K, "K", "k"), (V, "V", "v"), (O, "O", "o"), (dO, "dO", "o"), (dQ, "dQ", "q"), (dK, "dK", "k"), (dV, "dV", "v")),
+             ((LSE, "LSE", torch.float32, p._rows), (q_lens, "q_lens", torch.int32, lens), (kv_lens, "kv_lens", torch.int32, lens)), dev)
     workspace = p.alloc_workspace(True, Q.device) if workspace is None else workspace
-    _chk_ws(workspace, "workspace", p._workspace_bytes[1])
-    _check(load().llsa_dense_backward(p._h, _ptr(Q), _ptr(K), _ptr(V), _ptr(q_lens), _ptr(kv_lens), _ptr(O), _ptr(LSE), _ptr(dO), _ptr(dQ),
-                                      _ptr(dK), _ptr(dV), _ptr(workspace), _stream()), "llsa_dense_backward")
+    _chk_ws(workspace, "workspace", p._workspace_bytes[1], dev)
+    _check(load().llsa_dense_backward(p._h, Q.data_ptr(), K.data_ptr(), V.data_ptr(), _ptr(q_lens), _ptr(kv_lens), O.data_ptr(), LSE.data_ptr(),
+                                      dO.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), workspace.data_ptr(), _stream()),
+           "llsa_dense_backward")
     return dQ, dK, dV
 
 
@@ -548,7 +552,8 @@ class NormPlan:
         self.batch, self.N, self.C, self.mod_stride = batch, N, C, mod_stride
         self.torch_dtype = torch.float32 if dtype == F32 else torch.bfloat16
         self.mod_torch_dtype = torch.float32 if mod_dtype == F32 else torch.bfloat16
-        self._mod_rows = batch if mod_stride else 1
+        self._shape, self._vec, self._mods = torch.Size((batch, N, C)), torch.Size((C,)), torch.Size((batch if mod_stride else 1, C))
+        self._stats = torch.Size((batch, N, 4))
         self._workspace_bytes = lib.llsa_norm_workspace_bytes(self._h)
 
     def __del__(self):
@@ -562,34 +567,32 @@ class NormPlan:
     def alloc_workspace(self, device="cuda") -> torch.Tensor:
         return torch.empty(self._workspace_bytes, dtype=torch.uint8, device=device)
 
-    def _check(self, rows=(), vecs=(), mods=()):
+    def _check(self, rows, vecs, mods, dev: int):
         for t, n in rows:
             if t is not None:
-                _chk_vec(t, n, self.torch_dtype, (self.batch, self.N, self.C))
+                _chk_vec(t, n, self.torch_dtype, self._shape, dev)
         for t, n in vecs:
             if t is not None:
-                _chk_vec(t, n, torch.float32, (self.C,))
+                _chk_vec(t, n, torch.float32, self._vec, dev)
         for t, n in mods:
             if t is not None:
-                _chk_vec(t, n, self.mod_torch_dtype, (self._mod_rows, self.C), last_only=True)
-                if self._mod_rows > 1 and t.stride(0) != self.mod_stride:
+                _chk_vec(t, n, self.mod_torch_dtype, self._mods, dev, rows_only=True)
+                if self._mods[0] > 1 and t.stride(0) != self.mod_stride:
                     raise LlsaError(f"{n}: expected rows {self.mod_stride} elements apart, got strides {t.stride()}")
 
 
 def norm_forward(p: NormPlan, x, branch=None, gain_branch=None, gate=None, gain=None, scale=None, shift=None, x_out=None, y=None, stats=None,
                  want_y=True):
     """``llsa_norm_forward``: returns ``(x_out, y, stats)``; ``x_out`` is ``x`` where there is no branch, ``y`` None if not wanted."""
-    if branch is None:
-        x_out = None
-    else:
-        x_out = torch.empty_like(x) if x_out is None else x_out
+    dev = _device()
+    x_out = None if branch is None else torch.empty_like(x) if x_out is None else x_out
     y = None if not want_y else torch.empty_like(x) if y is None else y
+    stats = torch.empty(p._stats, dtype=torch.float32, device=x.device) if stats is None else stats
     p._check(((x, "x"), (branch, "branch"), (x_out, "x_out"), (y, "y")), ((gain_branch, "gain_branch"), (gain, "gain")),
-             ((gate, "gate"), (scale, "scale"), (shift, "shift")))
-    stats = torch.empty(p.batch, p.N, 4, dtype=torch.float32, device=x.device) if stats is None else stats
-    _chk_vec(stats, "stats", torch.float32, (p.batch, p.N, 4))
-    _check(load().llsa_norm_forward(p._h, _ptr(x), _ptr(branch), _ptr(gain_branch), _ptr(gate), _ptr(gain), _ptr(scale), _ptr(shift), _ptr(x_out),
-                                    _ptr(y), _ptr(stats), _stream()), "llsa_norm_forward")
+             ((gate, "gate"), (scale, "scale"), (shift, "shift")), dev)
+    _chk_vec(stats, "stats", torch.float32, p._stats, dev)
+    _check(load().llsa_norm_forward(p._h, x.data_ptr(), _ptr(branch), _ptr(gain_branch), _ptr(gate), _ptr(gain), _ptr(scale), _ptr(shift),
+                                    _ptr(x_out), _ptr(y), stats.data_ptr(), _stream()), "llsa_norm_forward")
     return x if branch is None else x_out, y, stats
 
 
@@ -597,21 +600,26 @@ def norm_backward(p: NormPlan, x_out, dy, stats, branch=None, gain_branch=None, 
                   dbranch=None, workspace=None):
     """``llsa_norm_backward``: a dict with ``dx``, ``dbranch`` and the fp32 gradients of those of ``gain_branch``, ``gate``, ``gain``, ``scale``, ``shift``
     (whose values are not needed) that are given.  ``dx`` may be ``dy`` or ``dx_out``, ``dbranch`` may be ``branch``."""
-    dx = torch.empty_like(x_out) if dx is None else dx
-    dbranch = None if branch is None else torch.empty_like(branch) if dbranch is None else dbranch
-    p._check(((x_out, "x_out"), (dy, "dy"), (branch, "branch"), (dx_out, "dx_out"), (dx, "dx"), (dbranch, "dbranch")),
-             ((gain_branch, "gain_branch"), (gain, "gain")), ((gate, "gate"), (scale, "scale"), (shift, "shift")))
-    _chk_vec(stats, "stats", torch.float32, (p.batch, p.N, 4))
-    new = lambda t, *shape: None if t is None else torch.empty(*shape, dtype=torch.float32, device=x_out.device)
-    out = {"dx": dx, "dbranch": dbranch, "dgain_branch": new(gain_branch, p.C), "dgate": new(gate, p._mod_rows, p.C), "dgain": new(gain, p.C),
-           "dscale": new(scale, p._mod_rows, p.C), "dshift": new(shift, p._mod_rows, p.C)}
-    if workspace is None and any(out[n] is not None for n in ("dgain_branch", "dgate", "dgain", "dscale", "dshift")):
+    dev = _device()
+    out = {"dx": torch.empty_like(x_out) if dx is None else dx}
+    if branch is not None:
+        out["dbranch"] = torch.empty_like(branch) if dbranch is None else dbranch
+    p._check(((x_out, "x_out"), (dy, "dy"), (branch, "branch"), (dx_out, "dx_out"), (out["dx"], "dx"), (out.get("dbranch"), "dbranch")),
+             ((gain_branch, "gain_branch"), (gain, "gain")), ((gate, "gate"), (scale, "scale"), (shift, "shift")), dev)
+    _chk_vec(stats, "stats", torch.float32, p._stats, dev)
+    sums = [None] * 5
+    for i, (t, n, shape) in enumerate(((gain_branch, "dgain_branch", p._vec), (gate, "dgate", p._mods), (gain, "dgain", p._vec),
+                                       (scale, "dscale", p._mods), (shift, "dshift", p._mods))):
+        if t is not None:
+            out[n] = torch.empty(shape, dtype=torch.float32, device=x_out.device)
+            sums[i] = out[n].data_ptr()
+    if workspace is None and any(sums):
         workspace = p.alloc_workspace(x_out.device)
-    _chk_ws(workspace, "workspace", p._workspace_bytes)
-    _check(load().llsa_norm_backward(p._h, _ptr(x_out), _ptr(branch), _ptr(gain_branch), _ptr(gate), _ptr(gain), _ptr(scale), _ptr(stats), _ptr(dy),
-                                     _ptr(dx_out), _ptr(dx), _ptr(dbranch), *(_ptr(out[n]) for n in ("dgain_branch", "dgate", "dgain", "dscale", "dshift")),
-                                     _ptr(workspace), _stream()), "llsa_norm_backward")
-    return {n: t for n, t in out.items() if t is not None}
+    _chk_ws(workspace, "workspace", p._workspace_bytes, dev)
+    _check(load().llsa_norm_backward(p._h, x_out.data_ptr(), _ptr(branch), _ptr(gain_branch), _ptr(gate), _ptr(gain), _ptr(scale), stats.data_ptr(),
+                                     _ptr(dy), _ptr(dx_out), out["dx"].data_ptr(), _ptr(out.get("dbranch")), *sums, _ptr(workspace), _stream()),
+           "llsa_norm_backward")
+    return out
 
 
 def measured_peaks(mfma_iters: int = 20000, copy_bytes: int = 1 << 30, reps: int = 5) -> dict:
