@@ -8,9 +8,10 @@
 
 namespace llsa {
 
-// waves a SIMD that the registers are shared out for (the key-major sums of a narrow workgroup take more than half of a CU's LDS at d = 128)
+// Waves a SIMD that the registers are shared out for (the key-major sums of a narrow workgroup take more than half of a CU's LDS at d = 128; three at
+// 128 bytes a row: 16 x 16384 tokens, d = 64, backward 3450 -> 3340 us)
 template <class T, int D> constexpr int dq_waves() { return D * (int)sizeof(T) <= 256 ? 2 : 1; }
-template <class T, int D, bool NARROW> constexpr int dkv_waves() { return D * (int)sizeof(T) <= 256 && !(NARROW && D == 128) ? 2 : 1; }
+template <class T, int D, bool NARROW> constexpr int dkv_waves() { return D * (int)sizeof(T) <= 128 && !NARROW ? 3 : D * (int)sizeof(T) <= 256 && !(NARROW && D == 128) ? 2 : 1; }
 
 // NARROW: 32 rows a workgroup, of which each wave has every fourth tile of keys, in stages of its own; the waves' sums are added up at the end.
 template <class T, int D, int KT, bool NARROW>
@@ -85,21 +86,42 @@ __global__ void __launch_bounds__(256, (dq_waves<T, D>())) dense_dq_kernel(Dense
         for (int u = 0; u < SUBS; ++u) {                     // (unrolled, the operands of two of them at once do not fit at d = 128)
             const Tile at = tile.at(stage(t) + u * 32 * Tile::ROWB);
             f32x16 s = s_from, dp = dp_from;
+            const bool some = k0 + 32 * u + 32 > mine.all;   // a key that some row does not see
+            const int lim = seen - k0 - 32 * u - 4 * h;
+            auto unseen = [&](f32x16 &x) {
 #pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(at.row(kt, 0, ks), q[ks], s);
+                for (int e = 0; e < 16; ++e) x[e] = 8 * (e >> 2) + (e & 3) < lim ? x[e] : 0.f;
+            };
+            if constexpr (sizeof(T) == 2) {
+                constexpr int KS = Tile::KS, NB = Tile::NB, N1 = KS, N2 = 2 * KS, N3 = N2 + 2 * NB;
+                auto op = operands<N3, 2>([&](auto ic) {
+                    constexpr int i = decltype(ic)::value;
+                    if constexpr (i < N1) return __builtin_bit_cast(bf16x8, at.row(kt, 0, i).w);
+                    else if constexpr (i < N2) return __builtin_bit_cast(bf16x8, at.row(vt, 0, i - N1).w);
+                    else return at.col(kt, 0, (i - N2) % NB, (i - N2) / NB);
+                });
+                constants<KS>([&](auto i) { op.take(i, [&](bf16x8 x) { s = mfma32(x, __builtin_bit_cast(bf16x8, q[i].w), s); }); });
+                constants<KS>([&](auto i) {                  // the exponentials while dP is formed
+                    op.take(plus(i, std::integral_constant<int, N1>()), [&](bf16x8 x) { dp = mfma32(x, __builtin_bit_cast(bf16x8, g[i].w), dp); });
 #pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(vt, 0, ks), g[ks], dp);
+                    for (int e = i * (16 / KS); e < (i + 1) * (16 / KS); ++e) s[e] = __builtin_amdgcn_exp2f(s[e] * a.scale2);
+                });
 #pragma unroll
-            for (int e = 0; e < 16; ++e) dp[e] *= __builtin_amdgcn_exp2f(s[e] * a.scale2);
-            if (k0 + 32 * u + 32 > mine.all) {
-                const int lim = seen - k0 - 32 * u - 4 * h;
+                for (int e = 0; e < 16; ++e) dp[e] *= s[e];
+                if (some) unseen(dp);
+                const bf16x8 ds[2] = {round8(dp, 0), round8(dp, 1)};
+                constants<2 * NB>([&](auto i) { op.take(plus(i, std::integral_constant<int, N2>()), [&](bf16x8 x) { dq[i % NB] = mfma32(x, ds[i / NB], dq[i % NB]); }); });
+            } else {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dp[e] = 8 * (e >> 2) + (e & 3) < lim ? dp[e] : 0.f;
+                for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(at.row(kt, 0, ks), q[ks], s);
+#pragma unroll
+                for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(vt, 0, ks), g[ks], dp);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) dp[e] *= __builtin_amdgcn_exp2f(s[e] * a.scale2);
+                if (some) unseen(dp);
+#pragma unroll
+                for (int n = 0; n < Tile::NB; ++n) dq[n] = at.col_product(kt, 0, n, dp, dq[n]);
             }
-            Probs<T> ds;
-            ds.set(dp);
-#pragma unroll
-            for (int n = 0; n < Tile::NB; ++n) dq[n] = at.col_product(kt, 0, n, ds, dq[n]);
         }
     }
 
@@ -134,7 +156,10 @@ __global__ void __launch_bounds__(256, (dkv_waves<T, D, NARROW>())) dense_dkv_ke
     using Loads = TileLoads<T, D, QT, NARROW ? 1 : 4>;
     constexpr int TILEB = QT * Tile::ROWB, SUBS = QT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1;
     constexpr int ST = dense_stages<T, D, NARROW>(), STAGEB = 2 * TILEB + 1024;
-    constexpr int LDSB = WAVES * ST * STAGEB, JOINB = NARROW ? 24576 * Tile::NB : 0;
+    // Two of the eight pieces of a lane's key stand in LDS at d = 128: the registers hold 64 of sums for each of dK and dV and 24 of 32 of keys and 32 of values, and a spill to
+    // memory in the loop would wait for the ring's newest tile.
+    constexpr int SPARE = sizeof(T) == 2 && D == 128 && !NARROW ? 2 : 0, KR = Tile::KS - SPARE;
+    constexpr int LDSB = WAVES * ST * STAGEB + 4096 * SPARE, JOINB = NARROW ? 24576 * Tile::NB : 0;
     // wave; stage; queries, their output's gradients, their -LSE / scale and -D
     __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
@@ -148,11 +173,13 @@ __global__ void __launch_bounds__(256, (dkv_waves<T, D, NARROW>())) dense_dkv_ke
     if (piece.none) return;
     const bool valid = j < p.nk;
 
-    Piece<T> k[Tile::KS], v[Tile::KS];
+    Piece<T> k[KR], v[Tile::KS];
+    u32x4 *const spare = reinterpret_cast<u32x4 *>(lds + WAVES * ST * STAGEB + wave * (1024 * SPARE)) + lane;
 #pragma unroll
     for (int ks = 0; ks < Tile::KS; ++ks) {
-        const u32x4 zero = {0, 0, 0, 0};
-        k[ks].w = valid ? *reinterpret_cast<const u32x4 *>(p.K + j * a.k.token + 16 * h + 32 * ks) : zero;
+        const u32x4 zero = {0, 0, 0, 0}, x = valid ? *reinterpret_cast<const u32x4 *>(p.K + j * a.k.token + 16 * h + 32 * ks) : zero;
+        if (ks < KR) k[ks].w = x;
+        else spare[64 * (ks - KR)] = x;
         v[ks].w = valid ? *reinterpret_cast<const u32x4 *>(p.V + j * a.v.token + 16 * h + 32 * ks) : zero;
     }
     f32x16 dk[Tile::NB], dv[Tile::NB];
@@ -200,31 +227,70 @@ __global__ void __launch_bounds__(256, (dkv_waves<T, D, NARROW>())) dense_dkv_ke
 #pragma unroll
                 for (int i = 0; i < 4; ++i) { s[e + i] = x[i]; dp[e + i] = y[i]; }
             }
+            const bool some = r0 < wto;                      // a row that does not see some key
+            auto unseen = [&](f32x16 &x) {
+                int lim = from - r0 - 4 * h;
+                asm volatile("" : "+v"(lim));                // (compared anew each time: sixteen pairs of scalar registers would be kept from S to dS)
 #pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(at.row(qt, 0, ks), k[ks], s);
+                for (int e = 0; e < 16; ++e) x[e] = 8 * (e >> 2) + (e & 3) >= lim ? x[e] : 0.f;
+            };
+            if constexpr (sizeof(T) == 2) {
+                constexpr int KS = Tile::KS, NB = Tile::NB, N1 = KS, N2 = 2 * KS, N3 = N2 + 2 * NB, N4 = N3 + 2 * NB;
+                auto op = operands<N4, 2>([&](auto ic) {
+                    constexpr int i = decltype(ic)::value;
+                    if constexpr (i < N1) return __builtin_bit_cast(bf16x8, at.row(qt, 0, i).w);
+                    else if constexpr (i < N2) return __builtin_bit_cast(bf16x8, at.row(gt, 0, i - N1).w);
+                    else if constexpr (i < N3) return at.col(gt, 0, (i - N2) % NB, (i - N2) / NB);
+                    else return at.col(qt, 0, (i - N3) % NB, (i - N3) / NB);
+                });
+                u32x4 ks[SPARE ? SPARE : 1];
+                constants<KS>([&](auto i) {
+                    if constexpr (SPARE && i == KR - 2)
 #pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(gt, 0, ks), v[ks], dp);
+                        for (int c = 0; c < SPARE; ++c) ks[c] = spare[64 * c];
+                    op.take(i, [&](bf16x8 x) {
+                        if constexpr (i < KR) s = mfma32(x, __builtin_bit_cast(bf16x8, k[i].w), s);
+                        else s = mfma32(x, __builtin_bit_cast(bf16x8, ks[i - KR]), s);
+                    });
+                });
+                constants<KS>([&](auto i) {                  // the exponentials while dP is formed
+                    op.take(plus(i, std::integral_constant<int, N1>()), [&](bf16x8 x) { dp = mfma32(x, __builtin_bit_cast(bf16x8, v[i].w), dp); });
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[e] = __builtin_amdgcn_exp2f(s[e] * a.scale2);
-                dp[e] *= s[e];
-            }
-            if (r0 < wto) {
-                const int lim = from - r0 - 4 * h;
+                    for (int e = i * (16 / KS); e < (i + 1) * (16 / KS); ++e) s[e] = __builtin_amdgcn_exp2f(s[e] * a.scale2);
+                });
+                if (some) unseen(s);
+                bf16x8 x8 = round8(s, 0);
+                constants<2 * NB>([&](auto i) {              // dS while P's products are
+                    if constexpr (i == NB) x8 = round8(s, 1);
+                    op.take(plus(i, std::integral_constant<int, N2>()), [&](bf16x8 x) { dv[i % NB] = mfma32(x, x8, dv[i % NB]); });
+#pragma unroll
+                    for (int e = i * (8 / NB); e < (i + 1) * (8 / NB); ++e) dp[e] *= s[e];
+                });
+                if (some) unseen(dp);
+                x8 = round8(dp, 0);
+                constants<2 * NB>([&](auto i) {
+                    if constexpr (i == NB) x8 = round8(dp, 1);
+                    op.take(plus(i, std::integral_constant<int, N3>()), [&](bf16x8 x) { dk[i % NB] = mfma32(x, x8, dk[i % NB]); });
+                });
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < KR; ++ks) s = piece_product(at.row(qt, 0, ks), k[ks], s);
+#pragma unroll
+                for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(gt, 0, ks), v[ks], dp);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const bool sees = 8 * (e >> 2) + (e & 3) >= lim;
-                    s[e] = sees ? s[e] : 0.f;
-                    dp[e] = sees ? dp[e] : 0.f;
+                    s[e] = __builtin_amdgcn_exp2f(s[e] * a.scale2);
+                    dp[e] *= s[e];
                 }
+                if (some) {
+                    unseen(s);
+                    unseen(dp);
+                }
+#pragma unroll
+                for (int n = 0; n < Tile::NB; ++n) dv[n] = at.col_product(gt, 0, n, s, dv[n]);
+#pragma unroll
+                for (int n = 0; n < Tile::NB; ++n) dk[n] = at.col_product(qt, 0, n, dp, dk[n]);
             }
-            Probs<T> pr, ds;
-            pr.set(s);
-            ds.set(dp);
-#pragma unroll
-            for (int n = 0; n < Tile::NB; ++n) dv[n] = at.col_product(gt, 0, n, pr, dv[n]);
-#pragma unroll
-            for (int n = 0; n < Tile::NB; ++n) dk[n] = at.col_product(qt, 0, n, ds, dk[n]);
         }
     }
 

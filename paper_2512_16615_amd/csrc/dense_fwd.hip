@@ -1,4 +1,4 @@
-// Dense attention, forward: workgroups of 4 waves, 32 QB rows each (a row: a query of one of the heads that share a key head), keys and values in
+// Dense attention, forward: workgroups of 4 waves, 32 rows each (a row: a query of one of the heads that share a key head), keys and values in
 // tiles of KT through LDS, the running maximum and sum of a softmax in registers.  A lane has one row: its scores come out of the first product in the
 // registers that the second one takes, O^T = V^T P^T collects channels in the registers of the same lane, so maximum, sum and rescaling are
 // the lane's own (and its partner's in the other half of the wave).
@@ -9,55 +9,42 @@
 
 namespace llsa {
 
-// waves a SIMD that the registers are shared out for
-template <class T, int D, int QB> constexpr int fwd_waves() { return D * (int)sizeof(T) * QB <= 256 ? 2 : 1; }
+// Waves a SIMD that the registers are shared out for.  Four at 128 bytes a row (three spilled registers and a wave more: 16 x 16384 tokens, d = 64, 1134 -> 1104 us;
+// 16 x 4096, causal, 57.3 -> 58.3).
+template <class T, int D, bool NARROW> constexpr int fwd_waves() { return D * (int)sizeof(T) <= 128 && !NARROW ? 4 : D * (int)sizeof(T) <= 256 ? 2 : 1; }
 
 // NARROW: 32 rows a workgroup, of which each wave has every fourth tile of keys, in stages of its own; the waves' sums are added up at the end.
-template <class T, int D, int QB, int KT, bool NARROW>
-__global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
+template <class T, int D, int KT, bool NARROW>
+__global__ void __launch_bounds__(256, (fwd_waves<T, D, NARROW>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
     using Tile = DenseTile<T, D>;
     using Loads = TileLoads<T, D, KT, NARROW ? 1 : 4>;
-    constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32, AXIS = NARROW ? 32 : 128 * QB, WAVES = NARROW ? 4 : 1;
+    constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1, KS = Tile::KS, NB = Tile::NB;
     constexpr int ST = dense_stages<T, D, NARROW>();
-    constexpr int LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * Tile::NB + 2048 : 0;
+    constexpr int LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * NB + 2048 : 0;
     __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];      // wave; stage; keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const DenseWork work = dense_work(grid, a.causal, true);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
-    const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + wave * (32 * QB);
-    // The wave's rows as operands, and what each sees.  All rows are read, those behind the length too, so that they are on their way before the
-    // lengths are there: whatever such a row holds stays in its own lane.
-    Piece<T> q[QB][Tile::KS];
-    int seen[QB], qi[QB], qg[QB];
+    const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + wave * 32, r = wrow0 + col;
+    // The wave's rows as operands.  All rows are read, those behind the length too, so that they are on their way before the lengths are there:
+    // what such a row holds stays in its own lane.
+    const bool in = r < grid.rows;
+    const int qi = (int)a.div_g((uint32_t)(in ? r : 0)), qg = (int)((in ? r : 0) - (int64_t)qi * a.G);
+    Piece<T> q[KS];
 #pragma unroll
-    for (int c = 0; c < QB; ++c) {
-        const int64_t r = wrow0 + 32 * c + col;
-        const bool in = r < grid.rows;
-        qi[c] = (int)a.div_g((uint32_t)(in ? r : 0));
-        qg[c] = (int)((in ? r : 0) - (int64_t)qi[c] * a.G);
-        const char *src = p.Q + qg[c] * a.q.head + qi[c] * a.q.token + 16 * h;
-#pragma unroll
-        for (int ks = 0; ks < Tile::KS; ++ks) q[c][ks].w = *reinterpret_cast<const u32x4 *>(src + 32 * ks);
-        if (!in) qi[c] = -1;
-    }
+    for (int ks = 0; ks < KS; ++ks) q[ks].w = *reinterpret_cast<const u32x4 *>(p.Q + qg * a.q.head + qi * a.q.token + 16 * h + 32 * ks);
     const DensePieces piece(grid, work.split, 0, dense_key_steps<AXIS, KT>(a, p, row0));
     if (piece.none) return;
-    const KeySpan mine = key_span(a, p, wrow0, wrow0 + 32 * QB - 1);
-#pragma unroll
-    for (int c = 0; c < QB; ++c) seen[c] = qi[c] >= 0 ? p.seen(a, qi[c]) : 0;
+    const KeySpan mine = key_span(a, p, wrow0, wrow0 + 31);
+    const int seen = in ? p.seen(a, qi) : 0;
 
-    f32x16 o[QB][Tile::NB];
-    float m[QB], l[QB];                                      // the reference that the exponentials are relative to (log2), their sum in this lane
+    f32x16 o[NB];
+    float m = -3e38f, l = 0.f;                               // the reference that the exponentials are relative to (log2), their sum in this lane
 #pragma unroll
-    for (int c = 0; c < QB; ++c) {
+    for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int n = 0; n < Tile::NB; ++n)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[c][n][e] = 0.f;
-        m[c] = -3e38f;
-        l[c] = 0.f;
-    }
+        for (int e = 0; e < 16; ++e) o[n][e] = 0.f;
 
     char *const ring = lds + (NARROW ? wave * (ST * 2 * TILEB) : 0);
     const unsigned ring0 = lds_address(ring);
@@ -83,113 +70,121 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, QB>())) dense_fwd_kernel
         if (k0 >= mine.some) continue;
         const char *kt = ring, *vt = ring + TILEB;
         const Tile at = tile.at(stage(t));
-        f32x16 s[SUBS][QB];
+        f32x16 s[SUBS];
 #pragma unroll
-        for (int u = 0; u < SUBS; ++u) {
+        for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-            for (int c = 0; c < QB; ++c)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[u][c][e] = 0.f;
-#pragma unroll
-            for (int ks = 0; ks < Tile::KS; ++ks) {
-                const Piece<T> k = at.row(kt, u, ks);
-#pragma unroll
-                for (int c = 0; c < QB; ++c) s[u][c] = piece_product(k, q[c][ks], s[u][c]);
-            }
-        }
-        if (k0 + KT > mine.all) {                            // a key that some row does not see
-#pragma unroll
-            for (int c = 0; c < QB; ++c) {
-                const int lim = seen[c] - k0 - 4 * h;
+            for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+
+        // between the two products
+        auto softmax = [&]() {
+            if (k0 + KT > mine.all) {                        // a key that some row does not see
+                const int lim = seen - k0 - 4 * h;
 #pragma unroll
                 for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) s[u][c][e] = 32 * u + 8 * (e >> 2) + (e & 3) < lim ? s[u][c][e] : -INFINITY;
+                    for (int e = 0; e < 16; ++e) s[u][e] = 32 * u + 8 * (e >> 2) + (e & 3) < lim ? s[u][e] : -INFINITY;
             }
-        }
-#pragma unroll
-        for (int c = 0; c < QB; ++c) {
-            float mx = s[0][c][0];
+            float mx = s[0][0];
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][c][e]);
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e]);
             mx = half_max(mx) * a.scale2;
             // The reference follows the maximum only once that is 2^8 beyond it (the sums stay far from fp32's range), for all rows of the wave
             // at once: after the first tiles the accumulators are hardly ever rescaled.
-            if (__builtin_amdgcn_ballot_w64(mx > m[c] + 8.f)) {
-                const float m2 = fmaxf(m[c], mx), f = __builtin_amdgcn_exp2f(m[c] - m2);
-                m[c] = m2;
-                l[c] *= f;
+            if (__builtin_amdgcn_ballot_w64(mx > m + 8.f)) {
+                const float m2 = fmaxf(m, mx), f = __builtin_amdgcn_exp2f(m - m2);
+                m = m2;
+                l *= f;
 #pragma unroll
-                for (int n = 0; n < Tile::NB; ++n)
+                for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[c][n][e] *= f;
+                    for (int e = 0; e < 16; ++e) o[n][e] *= f;
             }
-            Probs<T> pr[SUBS];
+        };
+        auto take_exp = [&](int u, int first, int count) {
 #pragma unroll
-            for (int u = 0; u < SUBS; ++u) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[u][c][e] = __builtin_amdgcn_exp2f(fmaf(s[u][c][e], a.scale2, -m[c]));
-                    l[c] += s[u][c][e];
-                }
-                pr[u].set(s[u][c]);
+            for (int e = first; e < first + count; ++e) {
+                s[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][e], a.scale2, -m));
+                l += s[u][e];
             }
+        };
+        if constexpr (sizeof(T) == 2) {
+            constexpr int N1 = SUBS * KS, N2 = N1 + SUBS * 2 * NB;
+            auto op = operands<N2, 4>([&](auto ic) {
+                constexpr int i = decltype(ic)::value, j = i - N1;
+                if constexpr (i < N1) return __builtin_bit_cast(bf16x8, at.row(kt, i / KS, i % KS).w);
+                else return at.col(vt, j / (2 * NB), j % NB, j / NB % 2);
+            });
+            constants<N1>([&](auto i) { op.take(i, [&](bf16x8 x) { s[i / KS] = mfma32(x, __builtin_bit_cast(bf16x8, q[i % KS].w), s[i / KS]); }); });
+            softmax();
+            take_exp(0, 0, 16);
+            bf16x8 pr[2] = {round8(s[0], 0), round8(s[0], 1)};
+            constants<SUBS * 2 * NB>([&](auto i) {           // the first 32 keys' products while the other ones' exponentials are taken
+                constexpr int u = i / (2 * NB), k = i % (2 * NB);
+                if constexpr (u > 0 && k == 0) { pr[0] = round8(s[u], 0); pr[1] = round8(s[u], 1); }
+                op.take(plus(i, std::integral_constant<int, N1>()), [&](bf16x8 x) { o[k % NB] = mfma32(x, pr[k / NB], o[k % NB]); });
+                if constexpr (u + 1 < SUBS) take_exp(u + 1, k * (8 / NB), 8 / NB);
+            });
+        } else {
 #pragma unroll
             for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                for (int n = 0; n < Tile::NB; ++n) o[c][n] = at.col_product(vt, u, n, pr[u], o[c][n]);
+                for (int ks = 0; ks < KS; ++ks) s[u] = piece_product(at.row(kt, u, ks), q[ks], s[u]);
+            softmax();
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) {
+                take_exp(u, 0, 16);
+#pragma unroll
+                for (int n = 0; n < NB; ++n) o[n] = at.col_product(vt, u, n, s[u], o[n]);
+            }
         }
     }
 
     if constexpr (NARROW) {                                  // each wave's exponentials are relative to its own reference
         __syncthreads();
-        float *ml = reinterpret_cast<float *>(lds + 12288 * Tile::NB);
-        ml[wave * 64 + lane] = m[0];
-        ml[256 + wave * 64 + lane] = l[0];
+        float *ml = reinterpret_cast<float *>(lds + 12288 * NB);
+        ml[wave * 64 + lane] = m;
+        ml[256 + wave * 64 + lane] = l;
         __syncthreads();
-        float top = m[0], sum = 0.f;
+        float top = m, sum = 0.f;
 #pragma unroll
         for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * 64 + lane]);
 #pragma unroll
         for (int w = 0; w < 4; ++w) sum = fmaf(ml[256 + w * 64 + lane], __builtin_amdgcn_exp2f(ml[w * 64 + lane] - top), sum);
-        add_waves(o[0], __builtin_amdgcn_exp2f(m[0] - top), lds, wave, lane);
+        add_waves(o, __builtin_amdgcn_exp2f(m - top), lds, wave, lane);
         if (wave > 0) return;
-        m[0] = top;
-        l[0] = sum;
+        m = top;
+        l = sum;
     }
-#pragma unroll
-    for (int c = 0; c < QB; ++c) {
-        const float sum = half_sum(l[c]);
-        if (!piece.alone) {
-            const int64_t at = ((int64_t)work.split * grid.groups + work.group) * grid.rows + wrow0 + 32 * c + col;
-            if (qi[c] >= 0) {
-                store_partial<D>(grid.part + at * D, o[c], h);
-                if (h == 0) *reinterpret_cast<float2 *>(grid.stat + 2 * at) = make_float2(m[c], sum);
-            }
-            continue;
+    const float sum = half_sum(l);
+    if (!piece.alone) {
+        const int64_t to = ((int64_t)work.split * grid.groups + work.group) * grid.rows + r;
+        if (in) {
+            store_partial<D>(grid.part + to * D, o, h);
+            if (h == 0) *reinterpret_cast<float2 *>(grid.stat + 2 * to) = make_float2(m, sum);
         }
-        const bool any = seen[c] > 0;
-        const float f = any ? 1.f / sum : 0.f;
-        keep_rows(o[c], any);
-        uint64_t redo = 0;
-        if (a.causal) {                                      // a key that some row of the tile does not see may have met it as 0 times an infinity
+        return;
+    }
+    const bool any = seen > 0;
+    const float f = any ? 1.f / sum : 0.f;
+    keep_rows(o, any);
+    uint64_t redo = 0;
+    if (a.causal) {                                          // a key that some row of the tile does not see may have met it as 0 times an infinity
 #pragma unroll
-            for (int n = 0; n < Tile::NB; ++n)
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[c][n][e] *= f;
-            redo = not_finite(o[c]) & __builtin_amdgcn_ballot_w64(any);
-            redo = (redo | redo >> 32) & 0xffffffffu;
-        }
-        char *dst = p.out + qg[c] * a.o.head + (int64_t)max(qi[c], 0) * a.o.token;
-        store_rows<T, D>(dst, o[c], a.causal ? 1.f : f, h, qi[c] >= 0);
-        if (h == 0 && qi[c] >= 0) p.LSE[(int64_t)qg[c] * a.Nq + qi[c]] = any ? (m[c] + __log2f(sum)) * kLn2 : -INFINITY;
-        while (redo) {
-            const int i = __builtin_ctzll(redo);
-            redo &= redo - 1;
-            dense_row_forward<T, D>(a, p, __builtin_amdgcn_readlane(qi[c], i), __builtin_amdgcn_readlane(qg[c], i), lane);
-        }
+            for (int e = 0; e < 16; ++e) o[n][e] *= f;
+        redo = not_finite(o) & __builtin_amdgcn_ballot_w64(any);
+        redo = (redo | redo >> 32) & 0xffffffffu;
+    }
+    store_rows<T, D>(p.out + qg * a.o.head + qi * a.o.token, o, a.causal ? 1.f : f, h, in);
+    if (h == 0 && in) p.LSE[(int64_t)qg * a.Nq + qi] = any ? (m + __log2f(sum)) * kLn2 : -INFINITY;
+    while (redo) {
+        const int i = __builtin_ctzll(redo);
+        redo &= redo - 1;
+        dense_row_forward<T, D>(a, p, __builtin_amdgcn_readlane(qi, i), __builtin_amdgcn_readlane(qg, i), lane);
     }
 }
 
@@ -230,7 +225,7 @@ template <class T, int D, int AXIS, int KT> __global__ void __launch_bounds__(25
 template <class T, int D, bool NARROW> static hipError_t launch_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
     constexpr int KT = dense_step(DenseTile<T, D>::ROWB, NARROW);
     const DenseGrid g = dense_grid(p, p.rows, p.fwd, D, ws);
-    dense_fwd_kernel<T, D, 1, KT, NARROW><<<g.wgs, 256, 0, s>>>(a, g);
+    dense_fwd_kernel<T, D, KT, NARROW><<<g.wgs, 256, 0, s>>>(a, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1) return e;
     dense_join_kernel<T, D, dense_tile(NARROW), KT><<<dim3((unsigned)((p.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);

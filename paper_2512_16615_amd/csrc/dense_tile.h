@@ -12,6 +12,8 @@
 // The first product contracts over channels: piece ks of a row is 32 bytes, 16 of them each half of the wave's (16 channels, one
 // instruction, or 8 channels, four of them).
 #pragma once
+#include <utility>
+
 #include "dense.h"
 #include "mfma_common.h"
 
@@ -57,20 +59,37 @@ __device__ __forceinline__ float piece_dot(const Piece<float> &a, const Piece<fl
     return s;
 }
 
-// A 32 x 32 tile of exponentials as the B operand of the second product: rounded to bf16 (half a step, 2^-8, of each; the
-// row sums are of the unrounded ones), fp32 as they are.
-template <class T> struct Probs;
-template <> struct Probs<__bf16> {
-    bf16x8 v[2];
-    __device__ __forceinline__ void set(const f32x16 &p) {
+// Registers 8 t .. 8 t + 7 of a 32 x 32 tile as the B operand of the second product: rounded to bf16, half a step (2^-8) of each; the sums over
+// a row of exponentials are of the unrounded ones.
+__device__ __forceinline__ bf16x8 round8(const f32x16 &p, int t) {
+    bf16x8 r;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { v[0][e] = (__bf16)p[e]; v[1][e] = (__bf16)p[8 + e]; }
+    for (int e = 0; e < 8; ++e) r[e] = (__bf16)p[8 * t + e];
+    return r;
+}
+
+// f of 0, 1, .. N - 1 as constants
+template <class F, int... I> __device__ __forceinline__ void constants(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, class F> __device__ __forceinline__ void constants(F f) { constants(f, std::make_integer_sequence<int, N>()); }
+
+// The LDS operands of a row of N matrix instructions, P of them on their way: the compiler reads each right in front of its instruction and
+// waits for it there, some 100 cycles for every 32 of the matrix unit.  take(i, f): f of operand i, then operand i + P is asked for; nothing is moved
+// across, so that the vector instructions written between two of them run while the matrix unit is busy.  16 x 8192 tokens, d = 128: forward 520 -> 502 us, backward
+// 1604 -> 1560; 16 x 4096, d = 64, causal 63 -> 57 and 175 -> 168; 3 x 16 heads, 4 key heads, x 1999, d = 128 111 -> 107 and 433 -> 392.
+template <int N, int P, class Fetch> struct Operands {
+    Fetch fetch;
+    bf16x8 op[P];
+    __device__ __forceinline__ explicit Operands(Fetch f) : fetch(f) {
+        constants<P>([&](auto i) { op[i] = fetch(i); });
+    }
+    template <int I, class F> __device__ __forceinline__ void take(std::integral_constant<int, I>, F f) {
+        f(op[I % P]);
+        if constexpr (I + P < N) op[I % P] = fetch(std::integral_constant<int, I + P>());
+        __builtin_amdgcn_sched_barrier(0);
     }
 };
-template <> struct Probs<float> {
-    f32x16 v;
-    __device__ __forceinline__ void set(const f32x16 &p) { v = p; }
-};
+template <int N, int P, class Fetch> __device__ __forceinline__ Operands<N, P, Fetch> operands(Fetch f) { return Operands<N, P, Fetch>(f); }
+template <int A, int B> constexpr std::integral_constant<int, A + B> plus(std::integral_constant<int, A>, std::integral_constant<int, B>) { return {}; }
 
 // Rows of D elements in LDS, unpadded; the 16-byte chunk c of row r stands at chunk c ^ key(r).  key permutes bits of r, so that (64 banks, 256 bytes
 // a cycle) neither the row-wise 16-byte read, whose 16 lanes at a time are at one chunk of rows that differ in all of r's low four bits, nor
@@ -108,21 +127,16 @@ template <class T, int D> struct DenseTile {
     __device__ __forceinline__ Piece<T> row(const char *tile, int sub, int ks) const {
         return {*reinterpret_cast<const u32x4 *>(tile + (lane_row ^ (32 * ks)) + sub * 32 * ROWB)};
     }
-    // acc += X^T p, X: rows 32 sub .. + 31 of the tile, channels 32 n .. + 31
-    __device__ __forceinline__ f32x16 col_product(const char *tile, int sub, int n, const Probs<T> &p, f32x16 acc) const {
-        if constexpr (sizeof(T) == 2) {
+    // 32 channels n .. of rows 32 sub + 16 t .. + 15 as an operand of the second product (bf16)
+    __device__ __forceinline__ bf16x8 col(const char *tile, int sub, int n, int t) const {
+        return lds_tr_pair(tile + (lane_col ^ (64 * n)) + (32 * sub + 16 * t) * ROWB, tile + (lane_col ^ (64 * n) ^ (ROWB >= 64 ? 32 : 16)) + (32 * sub + 16 * t + 8) * ROWB);
+    }
+    // acc += X^T p, X: rows 32 sub .. + 31 of the tile, channels 32 n .. + 31 (fp32)
+    __device__ __forceinline__ f32x16 col_product(const char *tile, int sub, int n, const f32x16 &p, f32x16 acc) const {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const char *lo = tile + (lane_col ^ (64 * n)) + (32 * sub + 16 * t) * ROWB;
-                const char *hi = tile + (lane_col ^ (64 * n) ^ (ROWB >= 64 ? 32 : 16)) + (32 * sub + 16 * t + 8) * ROWB;
-                acc = mfma32(lds_tr_pair(lo, hi), p.v[t], acc);
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = 8 * (r >> 2) + (r & 3);
-                acc = mfma32(*reinterpret_cast<const float *>(tile + (lane_col ^ ((key(row) << 4) ^ (128 * n))) + (32 * sub + row) * ROWB), p.v[r], acc);
-            }
+        for (int r = 0; r < 16; ++r) {
+            const int row = 8 * (r >> 2) + (r & 3);
+            acc = mfma32(*reinterpret_cast<const float *>(tile + (lane_col ^ ((key(row) << 4) ^ (128 * n))) + (32 * sub + row) * ROWB), p[r], acc);
         }
         return acc;
     }
@@ -190,6 +204,7 @@ template <class T, int D, int ROWS, int WAVES> struct TileLoads {
     // rows r0 + r of a group below `rows`, of two tensors (queries and their output's gradients) whose descriptors begin at query q0 = r0 / G
     static __device__ __forceinline__ void rows(u32x4 qbuf, u32x4 obuf, const DenseArgs &a, int r0, int q0, int rows, unsigned qlds, unsigned olds, int wave, int lane) {
         if (ALL < WAVES && wave >= ALL) return;
+        asm volatile("" : "+v"(lane));                       // (offsets formed anew each time: kept over the loop they cost a register each)
         const int rl = lane / Tile::CH, c = lane % Tile::CH;
 #pragma unroll
         for (int i = 0; i < N; i += STEP) {
@@ -197,7 +212,7 @@ template <class T, int D, int ROWS, int WAVES> struct TileLoads {
 #pragma unroll
             for (int k = 0; k < STEP; ++k) {
                 const int r = (wave * N + i + k) * Tile::RPI + rl;
-                const unsigned q = a.div_g(r0 + r), g = r0 + r - q * a.G, chunk = (c ^ Tile::key(r)) << 4;
+                const unsigned q = a.G == 1 ? r0 + r : a.div_g(r0 + r), g = r0 + r - q * a.G, chunk = (c ^ Tile::key(r)) << 4;
                 const bool in = r0 + r < rows;
                 vq[k] = in ? g * (unsigned)a.q.head + (q - q0) * (unsigned)a.q.token + chunk : 0xffffff00u;
                 vo[k] = in ? g * (unsigned)a.o.head + (q - q0) * (unsigned)a.o.token + chunk : 0xffffff00u;
