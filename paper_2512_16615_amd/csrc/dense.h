@@ -12,6 +12,10 @@ namespace llsa {
 
 struct DenseStrides { int64_t batch, head, token; };     // bytes
 
+// The forms of the tiled kernels: tiles of 128 rows (or keys) whose four waves have 32 each and walk over the other axis together; the same with eight waves, two for each 32, that
+// share out every tile of the other axis; tiles of 32 whose four waves share out the other axis itself.
+enum DenseForm { kDenseWide, kDensePaired, kDenseNarrow };
+
 // How a launch cuts its axis (rows, or keys) and the other one that each tile of it walks over
 struct DenseShape {
     bool narrow;                    // tiles of 32, whose four waves share out the other axis among themselves; else of 128, 32 a wave
@@ -75,6 +79,17 @@ size_t dense_part_bytes(const DensePlan &p, int64_t rows, const DenseShape &shap
 // tiles on the matrix instructions (dense_fwd.hip, dense_bwd.hip)
 hipError_t launch_dense_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s);
 hipError_t launch_dense_bwd(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s);
+
+// .. with the form that a launch takes
+bool dense_paired(const DensePlan &p, const DenseShape &shape, int64_t axis);
+template <class F> hipError_t dense_dispatch_form(const DensePlan &p, const DenseShape &shape, int64_t axis, F go) {
+    return dense_dispatch(p, [&](auto t, auto d) {
+        if (shape.narrow) return go(t, d, std::integral_constant<int, kDenseNarrow>());
+        if constexpr (dense_step(decltype(d)::value * (int)sizeof(t), false) == 64)
+            if (dense_paired(p, shape, axis)) return go(t, d, std::integral_constant<int, kDensePaired>());
+        return go(t, d, std::integral_constant<int, kDenseWide>());
+    });
+}
 
 // one wave a row (dense_row.hip)
 hipError_t launch_dense_fwd_rows(const DensePlan &p, const DenseArgs &a, hipStream_t s);

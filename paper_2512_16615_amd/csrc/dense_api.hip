@@ -38,22 +38,29 @@ static bool dense_apart(const DenseStrides &st, int64_t batch, int64_t heads, in
     return true;
 }
 
-// Tiles of 128 rows, each wave 32 of them, keep the matrix units busiest (the other axis is brought in once for all four); tiles of 32, whose waves share out the
-// other axis, are for what leaves half a tile or half the CUs empty otherwise.  The other axis is cut where there are fewer tiles than the CUs hold (two
-// workgroups each), not into pieces of less than 512 rows or keys: the partial sums are written and read once more.  Causal tiles differ, and the longest
-// alone takes as long as everything where all are resident at once; long ones are cut up to twice as many tiles (d = 64, 4 heads x 16384: 298 -> 243 us;
-// 16 x 4096, 64 steps of 64 keys, 74 -> 87).
+// Tiles of 128 rows (the other axis is brought in once for four waves' 32 each) keep the matrix units busiest; tiles of 32, whose waves share out the other axis, are for what
+// leaves half a tile or half the CUs empty otherwise.  The other axis is cut only where there are fewer tiles than CUs, not into pieces of less than 512 rows or
+// keys: the partial sums are written and read once more (16 x 2048 tokens, d = 64, 256 tiles: forward 47.8 us in two pieces, 26.3 in one).  Causal tiles differ, and the longest takes
+// as long as everything where all are resident at once: long ones are cut up to twice as many tiles (key tiles of 3 x 16 heads, 4 key heads, x 1999 tokens, d = 128, 125 steps:
+// backward 261 -> 182 us with lengths of 1999, 1500 and 700, 277 -> 263 without; 32 steps, 16 x 2048: 68.8 uncut, 86 in two).
 DenseShape dense_shape(const DensePlan &p, int64_t axis, int64_t other) {
     DenseShape r;
     const int64_t groups = (int64_t)p.desc.batch * p.desc.kv_heads, wide = groups * ((axis + 127) / 128), pieces = std::max<int64_t>(1, other / 512);
     r.narrow = axis <= 64 || wide * pieces < 128;
     const int step = dense_step(p.desc.d * p.elt, r.narrow);
     const int64_t tiles = r.narrow ? groups * ((axis + 31) / 32) : wide, steps = (other + step - 1) / step, least = 512 / step;
-    const bool differ = p.desc.causal && !r.narrow;
-    const int64_t target = differ && steps >= 128 ? 1024 : 512, want = tiles >= (differ ? target : 256) ? 1 : (target + tiles - 1) / tiles;
+    const int64_t target = r.narrow || (p.desc.causal && steps >= 96) ? 512 : 256;
+    const int64_t want = r.narrow ? (target + tiles - 1) / tiles : std::max<int64_t>(1, target / tiles);
     r.chunk = (int)std::max((steps + want - 1) / want, least);
     r.splits = (int)((steps + r.chunk - 1) / r.chunk);
     return r;
+}
+
+// Eight waves a tile, two for each 32 rows, where a CU has one tile anyway (8 x 4096 tokens, d = 128: forward 89 -> 70 us, backward 252 -> 219), or the longest of
+// causal tiles decides (16 x 4096, d = 64, 512 tiles: 60 -> 54 and 169 -> 151; 4 x 16384 212 -> 191 and 627 -> 513).  Beyond that two workgroups of four a CU do better: they
+// wait for each other less (756 tiles, d = 128: 58 us, paired 66).
+bool dense_paired(const DensePlan &p, const DenseShape &shape, int64_t axis) {
+    return (int64_t)p.desc.batch * p.desc.kv_heads * ((axis + 127) / 128) * shape.splits <= (p.desc.causal ? 512 : 256);
 }
 
 DenseGrid dense_grid(const DensePlan &p, int64_t rows, const DenseShape &shape, int row_floats, float *part) {

@@ -10,22 +10,26 @@ namespace llsa {
 
 // Waves a SIMD that the registers are shared out for (the key-major sums of a narrow workgroup take more than half of a CU's LDS at d = 128; three at
 // 128 bytes a row: 16 x 16384 tokens, d = 64, backward 3450 -> 3340 us)
-template <class T, int D> constexpr int dq_waves() { return D * (int)sizeof(T) <= 256 ? 2 : 1; }
-template <class T, int D, bool NARROW> constexpr int dkv_waves() { return D * (int)sizeof(T) <= 128 && !NARROW ? 3 : D * (int)sizeof(T) <= 256 && !(NARROW && D == 128) ? 2 : 1; }
+template <class T, int D, int FORM> constexpr int dq_waves() { return D * (int)sizeof(T) <= 256 || FORM == kDensePaired ? 2 : 1; }
+template <class T, int D, int FORM> constexpr int dkv_waves() {
+    return D * (int)sizeof(T) <= 128 && FORM == kDenseWide ? 3 : D * (int)sizeof(T) <= 256 && !(FORM == kDenseNarrow && D == 128) ? 2 : 1;
+}
 
-// NARROW: 32 rows a workgroup, of which each wave has every fourth tile of keys, in stages of its own; the waves' sums are added up at the end.
-template <class T, int D, int KT, bool NARROW>
-__global__ void __launch_bounds__(256, (dq_waves<T, D>())) dense_dq_kernel(DenseArgs a, DenseGrid grid) {
+// Narrow: each wave has every fourth tile of keys, in stages of its own.  Paired: the first or second half of every tile.  The waves' sums are added up at the end.
+template <class T, int D, int KT, int FORM>
+__global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dq_waves<T, D, FORM>())) dense_dq_kernel(DenseArgs a, DenseGrid grid) {
+    constexpr bool NARROW = FORM == kDenseNarrow, PAIRED = FORM == kDensePaired;
     using Tile = DenseTile<T, D>;
-    using Loads = TileLoads<T, D, KT, NARROW ? 1 : 4>;
+    using Loads = TileLoads<T, D, KT, NARROW ? 1 : PAIRED ? 8 : 4>;
     constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1;
-    constexpr int ST = dense_stages<T, D, NARROW>(), LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * Tile::NB : 0;
+    constexpr int ST = dense_stages<T, D, FORM>(), LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * Tile::NB : PAIRED ? 16384 * Tile::NB : 0;
     __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];      // wave; stage; keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
+    const int pair = wave & 3, half = wave >> 2;
     const DenseWork work = dense_work(grid, a.causal, true);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
-    const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + wave * 32, r = wrow0 + col;
+    const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + pair * 32, r = wrow0 + col;
     // All rows are read, those behind the length too, so that they are on their way before the lengths are there: what such a row holds stays in its lane.
     const bool in = r < grid.rows;
     const int qi = (int)a.div_g((uint32_t)(in ? r : 0)), qg = (int)((in ? r : 0) - (int64_t)qi * a.G);
@@ -46,7 +50,7 @@ __global__ void __launch_bounds__(256, (dq_waves<T, D>())) dense_dq_kernel(Dense
 #pragma unroll
     for (int ks = 0; ks < Tile::KS; ++ks) delta = piece_dot(g[ks], o[ks], delta);
     const float nD = seen > 0 ? -half_sum(delta) : 0.f, nlse = seen > 0 ? -lse / a.scale : -INFINITY;
-    if (work.split == 0 && h == 0 && (!NARROW || wave == 0)) {                         // also for the rows that the last tile has too many
+    if (work.split == 0 && h == 0 && (NARROW ? wave == 0 : half == 0)) {               // also for the rows that the last tile has too many
         a.nD[work.group * a.stat_rows + r] = nD;
         a.nlse[work.group * a.stat_rows + r] = nlse;
     }
@@ -83,7 +87,7 @@ __global__ void __launch_bounds__(256, (dq_waves<T, D>())) dense_dq_kernel(Dense
         if (k0 >= mine.some) continue;
         const char *kt = ring, *vt = ring + TILEB;
 #pragma unroll 1
-        for (int u = 0; u < SUBS; ++u) {                     // (unrolled, the operands of two of them at once do not fit at d = 128)
+        for (int u = PAIRED ? half : 0; u < SUBS; u += PAIRED ? 2 : 1) {      // (unrolled, the operands of two of them at once do not fit at d = 128)
             const Tile at = tile.at(stage(t) + u * 32 * Tile::ROWB);
             f32x16 s = s_from, dp = dp_from;
             const bool some = k0 + 32 * u + 32 > mine.all;   // a key that some row does not see
@@ -125,10 +129,11 @@ __global__ void __launch_bounds__(256, (dq_waves<T, D>())) dense_dq_kernel(Dense
         }
     }
 
-    if constexpr (NARROW) {
+    if constexpr (FORM != kDenseWide) {
         __syncthreads();
-        add_waves(dq, 1.f, lds, wave, lane);
-        if (wave > 0) return;
+        if (NARROW) add_waves(dq, 1.f, lds, wave, lane);
+        else add_halves(dq, 1.f, lds, pair, half, lane);
+        if (NARROW ? wave > 0 : half > 0) return;
     }
     if (!piece.alone) {
         if (in) store_partial<D>(grid.part + (((int64_t)work.split * grid.groups + work.group) * grid.rows + r) * D, dq, h);
@@ -149,24 +154,26 @@ __global__ void __launch_bounds__(256, (dq_waves<T, D>())) dense_dq_kernel(Dense
 }
 
 // A wave has 32 keys, theirs and their values' channels in registers, and walks over the rows (of every head that shares them) in tiles of QT.
-// NARROW: 32 keys a workgroup, for which each wave has every fourth tile of rows, in stages of its own.
-template <class T, int D, int QT, bool NARROW>
-__global__ void __launch_bounds__(256, (dkv_waves<T, D, NARROW>())) dense_dkv_kernel(DenseArgs a, DenseGrid grid) {
+// Narrow: 32 keys, for which each wave has every fourth tile of rows, in stages of its own.  Paired: the first or second half of every tile.
+template <class T, int D, int QT, int FORM>
+__global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dkv_waves<T, D, FORM>())) dense_dkv_kernel(DenseArgs a, DenseGrid grid) {
+    constexpr bool NARROW = FORM == kDenseNarrow, PAIRED = FORM == kDensePaired;
     using Tile = DenseTile<T, D>;
-    using Loads = TileLoads<T, D, QT, NARROW ? 1 : 4>;
+    using Loads = TileLoads<T, D, QT, NARROW ? 1 : PAIRED ? 8 : 4>;
     constexpr int TILEB = QT * Tile::ROWB, SUBS = QT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1;
-    constexpr int ST = dense_stages<T, D, NARROW>(), STAGEB = 2 * TILEB + 1024;
+    constexpr int ST = dense_stages<T, D, FORM>(), STAGEB = 2 * TILEB + 1024;
     // Two of the eight pieces of a lane's key stand in LDS at d = 128: the registers hold 64 of sums for each of dK and dV and 24 of 32 of keys and 32 of values, and a spill to
     // memory in the loop would wait for the ring's newest tile.
     constexpr int SPARE = sizeof(T) == 2 && D == 128 && !NARROW ? 2 : 0, KR = Tile::KS - SPARE;
-    constexpr int LDSB = WAVES * ST * STAGEB + 4096 * SPARE, JOINB = NARROW ? 24576 * Tile::NB : 0;
+    constexpr int LDSB = WAVES * ST * STAGEB + 4096 * SPARE, JOINB = NARROW ? 24576 * Tile::NB : PAIRED ? 16384 * Tile::NB : 0;
     // wave; stage; queries, their output's gradients, their -LSE / scale and -D
     __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
+    const int pair = wave & 3, half = wave >> 2;
     const DenseWork work = dense_work(grid, a.causal, false);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
-    const int key0 = work.tile * AXIS, wkey0 = NARROW ? key0 : key0 + wave * 32, j = wkey0 + col;
+    const int key0 = work.tile * AXIS, wkey0 = NARROW ? key0 : key0 + pair * 32, j = wkey0 + col;
     int first;
     const int steps = dense_row_steps<QT>(a, p, key0, &first);
     const DensePieces piece(grid, work.split, first, steps);
@@ -174,7 +181,7 @@ __global__ void __launch_bounds__(256, (dkv_waves<T, D, NARROW>())) dense_dkv_ke
     const bool valid = j < p.nk;
 
     Piece<T> k[KR], v[Tile::KS];
-    u32x4 *const spare = reinterpret_cast<u32x4 *>(lds + WAVES * ST * STAGEB + wave * (1024 * SPARE)) + lane;
+    u32x4 *const spare = reinterpret_cast<u32x4 *>(lds + WAVES * ST * STAGEB + pair * (1024 * SPARE)) + lane;
 #pragma unroll
     for (int ks = 0; ks < Tile::KS; ++ks) {
         const u32x4 zero = {0, 0, 0, 0}, x = valid ? *reinterpret_cast<const u32x4 *>(p.K + j * a.k.token + 16 * h + 32 * ks) : zero;
@@ -216,7 +223,7 @@ __global__ void __launch_bounds__(256, (dkv_waves<T, D, NARROW>())) dense_dkv_ke
         const char *qt = ring, *gt = ring + TILEB;
         const float *st = reinterpret_cast<const float *>(ring + stage(t) + 2 * TILEB);
 #pragma unroll 1
-        for (int u = 0; u < SUBS; ++u) {
+        for (int u = PAIRED ? half : 0; u < SUBS; u += PAIRED ? 2 : 1) {
             const int r0 = t * QT + 32 * u;
             if (r0 + 31 < wfrom) continue;
             const Tile at = tile.at(stage(t) + u * 32 * Tile::ROWB);
@@ -299,6 +306,12 @@ __global__ void __launch_bounds__(256, (dkv_waves<T, D, NARROW>())) dense_dkv_ke
         add_waves(dk, 1.f, lds, wave, lane);
         add_waves(dv, 1.f, lds + 12288 * Tile::NB, wave, lane);
         if (wave > 0) return;
+    } else if constexpr (PAIRED) {
+        __syncthreads();
+        add_halves(dk, 1.f, lds, pair, half, lane);
+        __syncthreads();
+        add_halves(dv, 1.f, lds, pair, half, lane);
+        if (half > 0) return;
     }
     if (!piece.alone) {
         float *to = grid.part + (((int64_t)work.split * grid.groups + work.group) * grid.rows + j) * (2 * D);
@@ -370,20 +383,22 @@ template <class T, int D, int AXIS, int QT> __global__ void __launch_bounds__(25
     dv.store(p.dV + j * a.v.token, lane);
 }
 
-template <class T, int D, bool NARROW> static hipError_t launch_dq(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
+template <class T, int D, int FORM> static hipError_t launch_dq(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
+    constexpr bool NARROW = FORM == kDenseNarrow;
     constexpr int KT = dense_step(DenseTile<T, D>::ROWB, NARROW);
     const DenseGrid g = dense_grid(p, p.rows, p.dq, D, part);
-    dense_dq_kernel<T, D, KT, NARROW><<<g.wgs, 256, 0, s>>>(a, g);
+    dense_dq_kernel<T, D, KT, FORM><<<g.wgs, FORM == kDensePaired ? 512 : 256, 0, s>>>(a, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1) return e;
     dense_dq_join_kernel<T, D, dense_tile(NARROW), KT><<<dim3((unsigned)((g.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);
     return hipGetLastError();
 }
 
-template <class T, int D, bool NARROW> static hipError_t launch_dkv(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
+template <class T, int D, int FORM> static hipError_t launch_dkv(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
+    constexpr bool NARROW = FORM == kDenseNarrow;
     constexpr int QT = dense_step(DenseTile<T, D>::ROWB, NARROW);
     const DenseGrid g = dense_grid(p, p.desc.Nkv, p.dkv, 2 * D, part);
-    dense_dkv_kernel<T, D, QT, NARROW><<<g.wgs, 256, 0, s>>>(a, g);
+    dense_dkv_kernel<T, D, QT, FORM><<<g.wgs, FORM == kDensePaired ? 512 : 256, 0, s>>>(a, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1) return e;
     dense_dkv_join_kernel<T, D, dense_tile(NARROW), QT><<<dim3((unsigned)((g.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);
@@ -391,13 +406,9 @@ template <class T, int D, bool NARROW> static hipError_t launch_dkv(const DenseP
 }
 
 hipError_t launch_dense_bwd(const DensePlan &p, const DenseArgs &a, float *part, hipStream_t s) {
-    return dense_dispatch(p, [&](auto t, auto d) {
-        using T = decltype(t);
-        constexpr int D = decltype(d)::value;
-        const hipError_t e = p.dq.narrow ? launch_dq<T, D, true>(p, a, part, s) : launch_dq<T, D, false>(p, a, part, s);
-        if (e != hipSuccess) return e;
-        return p.dkv.narrow ? launch_dkv<T, D, true>(p, a, part, s) : launch_dkv<T, D, false>(p, a, part, s);
-    });
+    const hipError_t e = dense_dispatch_form(p, p.dq, p.rows, [&](auto t, auto d, auto form) { return launch_dq<decltype(t), decltype(d)::value, decltype(form)::value>(p, a, part, s); });
+    if (e != hipSuccess) return e;
+    return dense_dispatch_form(p, p.dkv, p.desc.Nkv, [&](auto t, auto d, auto form) { return launch_dkv<decltype(t), decltype(d)::value, decltype(form)::value>(p, a, part, s); });
 }
 
 }  // namespace llsa

@@ -11,22 +11,24 @@ namespace llsa {
 
 // Waves a SIMD that the registers are shared out for.  Four at 128 bytes a row (three spilled registers and a wave more: 16 x 16384 tokens, d = 64, 1134 -> 1104 us;
 // 16 x 4096, causal, 57.3 -> 58.3).
-template <class T, int D, bool NARROW> constexpr int fwd_waves() { return D * (int)sizeof(T) <= 128 && !NARROW ? 4 : D * (int)sizeof(T) <= 256 ? 2 : 1; }
+template <class T, int D, int FORM> constexpr int fwd_waves() { return D * (int)sizeof(T) <= 128 && FORM == kDenseWide ? 4 : D * (int)sizeof(T) <= 256 ? 2 : 1; }
 
-// NARROW: 32 rows a workgroup, of which each wave has every fourth tile of keys, in stages of its own; the waves' sums are added up at the end.
-template <class T, int D, int KT, bool NARROW>
-__global__ void __launch_bounds__(256, (fwd_waves<T, D, NARROW>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
+// Narrow: each wave has every fourth tile of keys, in stages of its own.  Paired: the first or second half of every tile.  The waves' sums are added up at the end.
+template <class T, int D, int KT, int FORM>
+__global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (fwd_waves<T, D, FORM>())) dense_fwd_kernel(DenseArgs a, DenseGrid grid) {
+    constexpr bool NARROW = FORM == kDenseNarrow, PAIRED = FORM == kDensePaired;
     using Tile = DenseTile<T, D>;
-    using Loads = TileLoads<T, D, KT, NARROW ? 1 : 4>;
-    constexpr int TILEB = KT * Tile::ROWB, SUBS = KT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1, KS = Tile::KS, NB = Tile::NB;
-    constexpr int ST = dense_stages<T, D, NARROW>();
-    constexpr int LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * NB + 2048 : 0;
+    using Loads = TileLoads<T, D, KT, NARROW ? 1 : PAIRED ? 8 : 4>;
+    constexpr int TILEB = KT * Tile::ROWB, SUBS = PAIRED ? 1 : KT / 32, AXIS = dense_tile(NARROW), WAVES = NARROW ? 4 : 1, KS = Tile::KS, NB = Tile::NB;
+    constexpr int ST = dense_stages<T, D, FORM>();
+    constexpr int LDSB = WAVES * ST * 2 * TILEB, JOINB = NARROW ? 12288 * NB + 2048 : PAIRED ? 16384 * NB + 4096 : 0;
     __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];      // wave; stage; keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
+    const int pair = wave & 3, half = wave >> 2;
     const DenseWork work = dense_work(grid, a.causal, true);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
-    const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + wave * 32, r = wrow0 + col;
+    const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + pair * 32, r = wrow0 + col;
     // The wave's rows as operands.  All rows are read, those behind the length too, so that they are on their way before the lengths are there:
     // what such a row holds stays in its own lane.
     const bool in = r < grid.rows;
@@ -66,10 +68,10 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, NARROW>())) dense_fwd_ke
         if (NARROW) vm_wait<0>();                            // tile t is there (and nobody else reads the wave's stages),
         else vm_wait_barrier<0>();                           // for all waves, and nobody reads the other stage
         if (ST == 2 && t + WAVES < piece.t1) fetch(t + WAVES);
-        const int k0 = t * KT;
+        const int k0 = t * KT + (PAIRED ? half * 32 : 0);
         if (k0 >= mine.some) continue;
         const char *kt = ring, *vt = ring + TILEB;
-        const Tile at = tile.at(stage(t));
+        const Tile at = tile.at(stage(t) + (PAIRED ? half * 32 * Tile::ROWB : 0));
         f32x16 s[SUBS];
 #pragma unroll
         for (int u = 0; u < SUBS; ++u)
@@ -78,7 +80,7 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, NARROW>())) dense_fwd_ke
 
         // between the two products
         auto softmax = [&]() {
-            if (k0 + KT > mine.all) {                        // a key that some row does not see
+            if (k0 + 32 * SUBS > mine.all) {                        // a key that some row does not see
                 const int lim = seen - k0 - 4 * h;
 #pragma unroll
                 for (int u = 0; u < SUBS; ++u)
@@ -142,19 +144,23 @@ __global__ void __launch_bounds__(256, (fwd_waves<T, D, NARROW>())) dense_fwd_ke
         }
     }
 
-    if constexpr (NARROW) {                                  // each wave's exponentials are relative to its own reference
+    if constexpr (FORM != kDenseWide) {                      // each wave's exponentials are relative to its own reference
+        constexpr int N = NARROW ? 4 : 2, STEP = NARROW ? 1 : 4, ALL = NARROW ? 4 : 8;     // waves of a row, from one to the next; of the workgroup
         __syncthreads();
-        float *ml = reinterpret_cast<float *>(lds + 12288 * NB);
+        float *ml = reinterpret_cast<float *>(lds + (NARROW ? 12288 : 16384) * NB);
         ml[wave * 64 + lane] = m;
-        ml[256 + wave * 64 + lane] = l;
+        ml[(ALL + wave) * 64 + lane] = l;
         __syncthreads();
+        const int first = NARROW ? 0 : pair;
         float top = m, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[w * 64 + lane]);
+        for (int w = 0; w < N; ++w) top = fmaxf(top, ml[(first + w * STEP) * 64 + lane]);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) sum = fmaf(ml[256 + w * 64 + lane], __builtin_amdgcn_exp2f(ml[w * 64 + lane] - top), sum);
-        add_waves(o, __builtin_amdgcn_exp2f(m - top), lds, wave, lane);
-        if (wave > 0) return;
+        for (int w = 0; w < N; ++w) sum = fmaf(ml[(ALL + first + w * STEP) * 64 + lane], __builtin_amdgcn_exp2f(ml[(first + w * STEP) * 64 + lane] - top), sum);
+        const float f = __builtin_amdgcn_exp2f(m - top);
+        if (NARROW) add_waves(o, f, lds, wave, lane);
+        else add_halves(o, f, lds, pair, half, lane);
+        if (NARROW ? wave > 0 : half > 0) return;
         m = top;
         l = sum;
     }
@@ -222,10 +228,11 @@ template <class T, int D, int AXIS, int KT> __global__ void __launch_bounds__(25
     if (lane == 0) p.LSE[(int64_t)g * a.Nq + i] = any ? (m + __log2f(l)) * kLn2 : -INFINITY;
 }
 
-template <class T, int D, bool NARROW> static hipError_t launch_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
+template <class T, int D, int FORM> static hipError_t launch_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
+    constexpr bool NARROW = FORM == kDenseNarrow;
     constexpr int KT = dense_step(DenseTile<T, D>::ROWB, NARROW);
     const DenseGrid g = dense_grid(p, p.rows, p.fwd, D, ws);
-    dense_fwd_kernel<T, D, KT, NARROW><<<g.wgs, 256, 0, s>>>(a, g);
+    dense_fwd_kernel<T, D, KT, FORM><<<g.wgs, FORM == kDensePaired ? 512 : 256, 0, s>>>(a, g);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || g.splits == 1) return e;
     dense_join_kernel<T, D, dense_tile(NARROW), KT><<<dim3((unsigned)((p.rows + 3) / 4), g.groups), 256, 0, s>>>(a, g);
@@ -233,9 +240,7 @@ template <class T, int D, bool NARROW> static hipError_t launch_fwd(const DenseP
 }
 
 hipError_t launch_dense_fwd(const DensePlan &p, const DenseArgs &a, float *ws, hipStream_t s) {
-    return dense_dispatch(p, [&](auto t, auto d) {
-        return p.fwd.narrow ? launch_fwd<decltype(t), decltype(d)::value, true>(p, a, ws, s) : launch_fwd<decltype(t), decltype(d)::value, false>(p, a, ws, s);
-    });
+    return dense_dispatch_form(p, p.fwd, p.rows, [&](auto t, auto d, auto form) { return launch_fwd<decltype(t), decltype(d)::value, decltype(form)::value>(p, a, ws, s); });
 }
 
 }  // namespace llsa

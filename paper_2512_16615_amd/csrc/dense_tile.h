@@ -144,7 +144,7 @@ template <class T, int D> struct DenseTile {
 
 // Stages of a ring of two tensors' tiles.  A narrow workgroup's four rings have one each from 256 bytes a row: with two workgroups a CU the other one computes meanwhile
 // (one token of 32 heads, 8 key heads, d = 128, 8 sequences of 16384: 115 -> 110 us, of 500 to 16384: 69 -> 65).
-template <class T, int D, bool NARROW> constexpr int dense_stages() { return NARROW && DenseTile<T, D>::ROWB >= 256 ? 1 : 2; }
+template <class T, int D, int FORM> constexpr int dense_stages() { return FORM == kDenseNarrow && DenseTile<T, D>::ROWB >= 256 ? 1 : 2; }
 
 // Memory straight into LDS through a buffer descriptor: lane l fetches 16 bytes at its own offset, to 16 l of the 1024 bytes at `lds`; what lies
 // outside the descriptor's bytes arrives as zeros.  The asm begins with the wait states that a vector memory instruction needs behind a
@@ -247,6 +247,29 @@ template <int NB> __device__ __forceinline__ void add_waves(f32x16 (&acc)[NB], f
                     for (int w = 0; w < 3; ++w) x += buf[((w * NB + n) * 4 + k) * 64 + lane][e];
                     acc[n][4 * k + e] = x;
                 }
+    }
+}
+
+// The sums of two waves over the same rows, `half` 0's and 1's of pair `pair`, in the first.  lds: 16 KB a block.
+template <int NB> __device__ __forceinline__ void add_halves(f32x16 (&acc)[NB], float f, char *lds, int pair, int half, int lane) {
+    f32x4 *buf = reinterpret_cast<f32x4 *>(lds) + pair * NB * 256 + lane;
+    if (half) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                buf[(n * 4 + k) * 64] = f32x4{acc[n][4 * k] * f, acc[n][4 * k + 1] * f, acc[n][4 * k + 2] * f, acc[n][4 * k + 3] * f};
+    }
+    __syncthreads();
+    if (!half) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const f32x4 x = buf[(n * 4 + k) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[n][4 * k + e] = fmaf(acc[n][4 * k + e], f, x[e]);
+            }
     }
 }
 
