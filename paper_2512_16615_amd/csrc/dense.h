@@ -32,7 +32,7 @@ struct DensePlan {
     bool grads;                     // may gradients be written with the strides of Q, K and V?
     DenseShape fwd, dq, dkv;
     int64_t stat_rows;              // rows, rounded up to whole tiles
-    size_t nD_off, nlse_off;        // backward: -D = -rowsum(dO * O) and -LSE / scale of the rows of a group, [batch * kv_heads, stat_rows] fp32
+    size_t nD_off, nlse_off;        // backward: -D = -rowsum(dO * O) and the logsumexp (DenseArgs::nlse) of the rows of a group, [batch * kv_heads, stat_rows] fp32
     size_t part_off;                // backward: partial sums of split tiles
     size_t ws_fwd, ws_bwd;
 };
@@ -51,7 +51,7 @@ struct DenseArgs {
     char *out, *dQ, *dK, *dV;
     DenseStrides q, k, v, o;
     const int32_t *q_lens, *kv_lens;
-    float *LSE, *nD, *nlse;
+    float *LSE, *nD, *nlse;         // nlse: -LSE / scale (bf16) or -LSE log2 e (fp32)
     int64_t stat_rows;
     int64_t Nq, Nkv;
     int32_t kv_heads, G, causal;

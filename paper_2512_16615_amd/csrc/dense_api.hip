@@ -126,7 +126,7 @@ static llsa_status build_dense_plan(const llsa_dense_desc &d, DensePlan &p) {
     p.nD_off = 0;
     p.nlse_off = stat;
     p.part_off = 2 * stat;
-    p.ws_bwd = p.part_off + std::max(dense_part_bytes(p, p.rows, p.dq, d.d), dense_part_bytes(p, d.Nkv, p.dkv, 2 * d.d));
+    p.ws_bwd = p.part_off + std::max(dense_part_bytes(p, p.rows, p.dq, d.d + 1), dense_part_bytes(p, d.Nkv, p.dkv, 2 * d.d));
     return LLSA_OK;
 }
 

@@ -1,7 +1,8 @@
 // Dense attention, backward, in two launches that recompute the probabilities from the logsumexp and write each result once (no atomics, so the
 // same bits from call to call; S and dP are formed twice, 14 d operations a pair of a query and a key where 10 d would do):
 //   query-major: dQ = scale dS K, and D = rowsum(dO O), which the other one needs;   key-major: dV = P^T dO, dK = scale dS^T Q
-// with P = exp(S - LSE), dS = P (dO V^T - D).  -LSE / scale and -D are where the first products' sums begin, so P = exp2(scale2 S') and dS = P dP'.
+// with P = exp(S - LSE), dS = P (dO V^T - D).  -LSE / scale and -D are where the first products' sums begin, so P = exp2(scale2 S') and dS = P dP'.  In fp32 S begins
+// at 0 and LSE is subtracted where the exponential is taken: LSE / scale is some 100, whose last bit is more than S's own error.
 // P and dS enter the second products rounded to the I/O type (bf16: half a step, 2^-8, of each; sums are fp32).
 #include "dense_row.h"
 #include "dense_tile.h"
@@ -49,16 +50,18 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dq_waves<T,
     float delta = 0.f;
 #pragma unroll
     for (int ks = 0; ks < Tile::KS; ++ks) delta = piece_dot(g[ks], o[ks], delta);
-    const float nD = seen > 0 ? -half_sum(delta) : 0.f, nlse = seen > 0 ? -lse / a.scale : -INFINITY;
-    if (work.split == 0 && h == 0 && (NARROW ? wave == 0 : half == 0)) {               // also for the rows that the last tile has too many
+    float nD = seen > 0 ? -half_sum(delta) : 0.f;
+    constexpr bool ROUNDED = sizeof(T) == 2;
+    const float nlse = seen > 0 ? (ROUNDED ? -lse / a.scale : -lse * kLog2e) : -INFINITY;
+    const bool first = h == 0 && (NARROW ? wave == 0 : half == 0);
+    if (work.split == 0 && first) {                          // also for the rows that the last tile has too many
         a.nD[work.group * a.stat_rows + r] = nD;
         a.nlse[work.group * a.stat_rows + r] = nlse;
     }
-    f32x16 s_from, dp_from, dq[Tile::NB];
+    f32x16 s_from, dq[Tile::NB];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        s_from[e] = nlse;
-        dp_from[e] = nD;
+        s_from[e] = ROUNDED ? nlse : 0.f;
 #pragma unroll
         for (int n = 0; n < Tile::NB; ++n) dq[n][e] = 0.f;
     }
@@ -73,6 +76,30 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dq_waves<T,
         Loads::keys(buffer_of(p.K + k0 * a.k.token, (left - 1) * kt + Tile::ROWB), kt, to, NARROW ? 0 : wave, lane);
         Loads::keys(buffer_of(p.V + k0 * a.v.token, (left - 1) * vt + Tile::ROWB), vt, to + TILEB, NARROW ? 0 : wave, lane);
     };
+    // a row's sum over its lanes and waves, in all of them (the ring is free)
+    auto row_sum = [&](float x) {
+        x = half_sum(x);
+        if constexpr (FORM != kDenseWide) {
+            float *red = reinterpret_cast<float *>(lds);
+            __syncthreads();
+            red[wave * 64 + lane] = x;
+            __syncthreads();
+            x = red[(NARROW ? 0 : pair) * 64 + lane] + red[(NARROW ? 1 : pair + 4) * 64 + lane];
+            if (NARROW) x += red[128 + lane] + red[192 + lane];
+            __syncthreads();
+        }
+        return x;
+    };
+    // D of rowsum(dO O) is off by what O's rounding to bf16 left out: of a row of few keys as much as dS is by its own.  sum_j dS_ij = D - D' for the D' that dS was formed
+    // with, so the walk over the keys gives D itself: to the key-major pass always, and where it is short (512 keys: beyond them O is small beside dP) to a second walk that
+    // forms dQ.  Error of dQ and dK against 64 bits, causal 3 x 16 heads of up to 1999 tokens, d = 128: 2.5e-3 -> 2.4e-3 (1.7e-3 is the results' own rounding).
+    float sum = 0.f;                                         // of the lane's dS
+    const bool two = ROUNDED && piece.alone && (piece.t1 - piece.t0) * KT <= 512;
+#pragma unroll 1
+    for (int walk = two ? 0 : 1; walk < 2; ++walk) {
+    f32x16 dp_from;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dp_from[e] = nD;
     if (ST == 2 && t0 < piece.t1) fetch(t0);
     loads_done();
     for (int t = t0; t < piece.t1; t += WAVES) {
@@ -113,6 +140,9 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dq_waves<T,
 #pragma unroll
                 for (int e = 0; e < 16; ++e) dp[e] *= s[e];
                 if (some) unseen(dp);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum += dp[e];
+                if (walk == 0) continue;
                 const bf16x8 ds[2] = {round8(dp, 0), round8(dp, 1)};
                 constants<2 * NB>([&](auto i) { op.take(plus(i, std::integral_constant<int, N2>()), [&](bf16x8 x) { dq[i % NB] = mfma32(x, ds[i / NB], dq[i % NB]); }); });
             } else {
@@ -121,7 +151,7 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dq_waves<T,
 #pragma unroll
                 for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(vt, 0, ks), g[ks], dp);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dp[e] *= __builtin_amdgcn_exp2f(s[e] * a.scale2);
+                for (int e = 0; e < 16; ++e) dp[e] *= __builtin_amdgcn_exp2f(fmaf(s[e], a.scale2, nlse));
                 if (some) unseen(dp);
 #pragma unroll
                 for (int n = 0; n < Tile::NB; ++n) dq[n] = at.col_product(kt, 0, n, dp, dq[n]);
@@ -129,6 +159,22 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dq_waves<T,
         }
     }
 
+    if (walk == 0) {
+        nD = seen > 0 ? nD - row_sum(sum) : 0.f;
+        sum = 0.f;
+        if (FORM == kDenseWide) __syncthreads();             // nobody reads the ring that the second walk begins to fill
+    }
+    }
+
+    if constexpr (ROUNDED) {
+        sum = row_sum(sum);
+        if (piece.alone) {
+            nD = seen > 0 ? nD - sum : 0.f;
+            if (in && first) a.nD[work.group * a.stat_rows + r] = nD;
+        } else if (in && first) {
+            grid.stat[((int64_t)work.split * grid.groups + work.group) * grid.rows + r] = sum;
+        }
+    }
     if constexpr (FORM != kDenseWide) {
         __syncthreads();
         if (NARROW) add_waves(dq, 1.f, lds, wave, lane);
@@ -280,13 +326,16 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dkv_waves<T
                     op.take(plus(i, std::integral_constant<int, N3>()), [&](bf16x8 x) { dk[i % NB] = mfma32(x, x8, dk[i % NB]); });
                 });
             } else {
+                const f32x16 nlse16 = s;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
                 for (int ks = 0; ks < KR; ++ks) s = piece_product(at.row(qt, 0, ks), k[ks], s);
 #pragma unroll
                 for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(gt, 0, ks), v[ks], dp);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    s[e] = __builtin_amdgcn_exp2f(s[e] * a.scale2);
+                    s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale2, nlse16[e]));
                     dp[e] *= s[e];
                 }
                 if (some) {
@@ -348,11 +397,19 @@ template <class T, int D, int AXIS, int KT> __global__ void __launch_bounds__(25
     const int steps = dense_key_steps<AXIS, KT>(a, p, r / AXIS * AXIS), pieces = (steps + grid.chunk - 1) / grid.chunk;
     if (pieces <= 1) return;
     Row acc = Row::zero();
-    const int64_t step = (int64_t)grid.groups * grid.rows * D;
-    if (p.seen(a, i) > 0)
-        for (int s = 0; s < pieces; s += 64) acc.add_parts(grid.part + ((int64_t)blockIdx.y * grid.rows + r) * D + s * step, step, min(64, pieces - s), 1.f, lane);
+    const int64_t at = (int64_t)blockIdx.y * grid.rows + r, step = (int64_t)grid.groups * grid.rows;      // piece 0's sums; from piece to piece
+    float nD = a.nD[blockIdx.y * a.stat_rows + r];
+    if (p.seen(a, i) > 0) {
+        for (int s = 0; s < pieces; s += 64) acc.add_parts(grid.part + (at + s * step) * D, step * D, min(64, pieces - s), 1.f, lane);
+        if constexpr (sizeof(T) == 2) {
+            float sum = 0.f;
+            for (int s = lane; s < pieces; s += 64) sum += grid.stat[at + s * step];
+            nD -= wave_sum(sum);
+            if (lane == 0) a.nD[blockIdx.y * a.stat_rows + r] = nD;
+        }
+    }
     acc.scale(a.scale);
-    if (a.causal && !acc.finite()) dense_row_dq<T, D>(a, p, i, g, a.nD[blockIdx.y * a.stat_rows + r], lane);
+    if (a.causal && !acc.finite()) dense_row_dq<T, D>(a, p, i, g, nD, lane);
     else acc.store(p.dQ + g * a.q.head + i * a.q.token, lane);
 }
 
