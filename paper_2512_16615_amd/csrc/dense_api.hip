@@ -93,10 +93,10 @@ static llsa_status build_dense_plan(const llsa_dense_desc &d, DensePlan &p) {
     if (d.d != 16 && d.d != 32 && d.d != 64 && d.d != 128) return LLSA_ERR_UNSUPPORTED;
     if ((d.causal != 0 && d.causal != 1) || (d.kernel_path != 0 && d.kernel_path != 1)) return LLSA_ERR_UNSUPPORTED;
     p.G = d.heads / d.kv_heads;
-    if ((int64_t)d.batch * d.kv_heads * ((d.Nq * p.G + 31) / 32 + (d.Nkv + 31) / 32) >= ((int64_t)1 << 29)) return LLSA_ERR_UNSUPPORTED;   // launch grids
     // rows and keys are counted in 31 bits, groups are the grid's second dimension
     if (d.Nq > ((int64_t)1 << 30) || d.Nkv > ((int64_t)1 << 30) || d.Nq * p.G > ((int64_t)1 << 30)) return LLSA_ERR_UNSUPPORTED;
     if ((int64_t)d.batch * d.kv_heads > 65535) return LLSA_ERR_UNSUPPORTED;
+    if ((int64_t)d.batch * d.kv_heads * ((d.Nq * p.G + 31) / 32 + (d.Nkv + 31) / 32) >= ((int64_t)1 << 29)) return LLSA_ERR_UNSUPPORTED;   // launch grids
     p.rows = d.Nq * p.G;
     p.elt = d.dtype == LLSA_F32 ? 4 : 2;
     p.scale = d.sm_scale > 0.f ? d.sm_scale : (float)(1.0 / sqrt((double)d.d));

@@ -97,73 +97,74 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dq_waves<T,
     const bool two = ROUNDED && piece.alone && (piece.t1 - piece.t0) * KT <= 512;
 #pragma unroll 1
     for (int walk = two ? 0 : 1; walk < 2; ++walk) {
-    f32x16 dp_from;
+        f32x16 dp_from;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) dp_from[e] = nD;
-    if (ST == 2 && t0 < piece.t1) fetch(t0);
-    loads_done();
-    for (int t = t0; t < piece.t1; t += WAVES) {
-        if (ST == 1) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            fetch(t);
-        }
-        if (NARROW) vm_wait<0>();                            // tile t is there (and nobody else reads the wave's stages),
-        else vm_wait_barrier<0>();                           // for all waves, and nobody reads the other stage
-        if (ST == 2 && t + WAVES < piece.t1) fetch(t + WAVES);
-        const int k0 = t * KT;
-        if (k0 >= mine.some) continue;
-        const char *kt = ring, *vt = ring + TILEB;
+        for (int e = 0; e < 16; ++e) dp_from[e] = nD;
+        if (ST == 2 && t0 < piece.t1) fetch(t0);
+        loads_done();
+        for (int t = t0; t < piece.t1; t += WAVES) {
+            if (ST == 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                fetch(t);
+            }
+            if (NARROW) vm_wait<0>();                            // tile t is there (and nobody else reads the wave's stages),
+            else vm_wait_barrier<0>();                           // for all waves, and nobody reads the other stage
+            if (ST == 2 && t + WAVES < piece.t1) fetch(t + WAVES);
+            const int k0 = t * KT;
+            if (k0 >= mine.some) continue;
+            const char *kt = ring, *vt = ring + TILEB;
 #pragma unroll 1
-        for (int u = PAIRED ? half : 0; u < SUBS; u += PAIRED ? 2 : 1) {      // (unrolled, the operands of two of them at once do not fit at d = 128)
-            const Tile at = tile.at(stage(t) + u * 32 * Tile::ROWB);
-            f32x16 s = s_from, dp = dp_from;
-            const bool some = k0 + 32 * u + 32 > mine.all;   // a key that some row does not see
-            const int lim = seen - k0 - 32 * u - 4 * h;
-            auto unseen = [&](f32x16 &x) {
+            for (int u = PAIRED ? half : 0; u < SUBS; u += PAIRED ? 2 : 1) {      // (unrolled, the operands of two of them at once do not fit at d = 128)
+                const Tile at = tile.at(stage(t) + u * 32 * Tile::ROWB);
+                f32x16 s = s_from, dp = dp_from;
+                const bool some = k0 + 32 * u + 32 > mine.all;   // a key that some row does not see
+                const int lim = seen - k0 - 32 * u - 4 * h;
+                auto unseen = [&](f32x16 &x) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = 8 * (e >> 2) + (e & 3) < lim ? x[e] : 0.f;
-            };
-            if constexpr (sizeof(T) == 2) {
-                constexpr int KS = Tile::KS, NB = Tile::NB, N1 = KS, N2 = 2 * KS, N3 = N2 + 2 * NB;
-                auto op = operands<N3, 2>([&](auto ic) {
-                    constexpr int i = decltype(ic)::value;
-                    if constexpr (i < N1) return __builtin_bit_cast(bf16x8, at.row(kt, 0, i).w);
-                    else if constexpr (i < N2) return __builtin_bit_cast(bf16x8, at.row(vt, 0, i - N1).w);
-                    else return at.col(kt, 0, (i - N2) % NB, (i - N2) / NB);
-                });
-                constants<KS>([&](auto i) { op.take(i, [&](bf16x8 x) { s = mfma32(x, __builtin_bit_cast(bf16x8, q[i].w), s); }); });
-                constants<KS>([&](auto i) {                  // the exponentials while dP is formed
-                    op.take(plus(i, std::integral_constant<int, N1>()), [&](bf16x8 x) { dp = mfma32(x, __builtin_bit_cast(bf16x8, g[i].w), dp); });
+                    for (int e = 0; e < 16; ++e) x[e] = 8 * (e >> 2) + (e & 3) < lim ? x[e] : 0.f;
+                };
+                if constexpr (sizeof(T) == 2) {
+                    constexpr int KS = Tile::KS, NB = Tile::NB, N1 = KS, N2 = 2 * KS, N3 = N2 + 2 * NB;
+                    auto op = operands<N3, 2>([&](auto ic) {
+                        constexpr int i = decltype(ic)::value;
+                        if constexpr (i < N1) return __builtin_bit_cast(bf16x8, at.row(kt, 0, i).w);
+                        else if constexpr (i < N2) return __builtin_bit_cast(bf16x8, at.row(vt, 0, i - N1).w);
+                        else return at.col(kt, 0, (i - N2) % NB, (i - N2) / NB);
+                    });
+                    constants<KS>([&](auto i) { op.take(i, [&](bf16x8 x) { s = mfma32(x, __builtin_bit_cast(bf16x8, q[i].w), s); }); });
+                    constants<KS>([&](auto i) {                  // the exponentials while dP is formed
+                        op.take(plus(i, std::integral_constant<int, N1>()), [&](bf16x8 x) { dp = mfma32(x, __builtin_bit_cast(bf16x8, g[i].w), dp); });
 #pragma unroll
-                    for (int e = i * (16 / KS); e < (i + 1) * (16 / KS); ++e) s[e] = __builtin_amdgcn_exp2f(s[e] * a.scale2);
-                });
+                        for (int e = i * (16 / KS); e < (i + 1) * (16 / KS); ++e) s[e] = __builtin_amdgcn_exp2f(s[e] * a.scale2);
+                    });
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dp[e] *= s[e];
-                if (some) unseen(dp);
+                    for (int e = 0; e < 16; ++e) dp[e] *= s[e];
+                    if (some) unseen(dp);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum += dp[e];
-                if (walk == 0) continue;
-                const bf16x8 ds[2] = {round8(dp, 0), round8(dp, 1)};
-                constants<2 * NB>([&](auto i) { op.take(plus(i, std::integral_constant<int, N2>()), [&](bf16x8 x) { dq[i % NB] = mfma32(x, ds[i / NB], dq[i % NB]); }); });
-            } else {
+                    for (int e = 0; e < 16; ++e) sum += dp[e];
+                    if (walk == 0) continue;
+                    const bf16x8 ds[2] = {round8(dp, 0), round8(dp, 1)};
+                    constants<2 * NB>([&](auto i) { op.take(plus(i, std::integral_constant<int, N2>()), [&](bf16x8 x) { dq[i % NB] = mfma32(x, ds[i / NB], dq[i % NB]); }); });
+                } else {
 #pragma unroll
-                for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(at.row(kt, 0, ks), q[ks], s);
+                    for (int ks = 0; ks < Tile::KS; ++ks) s = piece_product(at.row(kt, 0, ks), q[ks], s);
 #pragma unroll
-                for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(vt, 0, ks), g[ks], dp);
+                    for (int ks = 0; ks < Tile::KS; ++ks) dp = piece_product(at.row(vt, 0, ks), g[ks], dp);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) dp[e] *= __builtin_amdgcn_exp2f(fmaf(s[e], a.scale2, nlse));
-                if (some) unseen(dp);
+                    for (int e = 0; e < 16; ++e) dp[e] *= __builtin_amdgcn_exp2f(fmaf(s[e], a.scale2, nlse));
+                    if (some) unseen(dp);
 #pragma unroll
-                for (int n = 0; n < Tile::NB; ++n) dq[n] = at.col_product(kt, 0, n, dp, dq[n]);
+                    for (int n = 0; n < Tile::NB; ++n) dq[n] = at.col_product(kt, 0, n, dp, dq[n]);
+                }
             }
         }
-    }
 
-    if (walk == 0) {
-        nD = seen > 0 ? nD - row_sum(sum) : 0.f;
-        sum = 0.f;
-        if (FORM == kDenseWide) __syncthreads();             // nobody reads the ring that the second walk begins to fill
-    }
+        if (walk == 0) {
+            const float all = row_sum(sum);                      // (barriers: for the waves without rows too)
+            nD = seen > 0 ? nD - all : 0.f;
+            sum = 0.f;
+            if (FORM == kDenseWide) __syncthreads();             // nobody reads the ring that the second walk begins to fill
+        }
     }
 
     if constexpr (ROUNDED) {
@@ -271,7 +272,7 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dkv_waves<T
 #pragma unroll 1
         for (int u = PAIRED ? half : 0; u < SUBS; u += PAIRED ? 2 : 1) {
             const int r0 = t * QT + 32 * u;
-            if (r0 + 31 < wfrom) continue;
+            if (r0 + 31 < wfrom || r0 >= rows) continue;     // (without rows: nobody wrote their -LSE and -D, where the other kernel's tiles are narrow)
             const Tile at = tile.at(stage(t) + u * 32 * Tile::ROWB);
             f32x16 s, dp;
 #pragma unroll

@@ -119,6 +119,16 @@ CASES = [
     _case("bf16", 1, 4, 4, 1024, 1024, 64), _case("bf16", 1, 4, 2, 1000, 1100, 128, causal=True), _case("f32", 1, 2, 2, 512, 512, 64), _case("bf16", 1, 2, 2, 700, 700, 32), _case("bf16", 1, 2, 2, 600, 600, 16, causal=True),
     # a sharp softmax: scores of tens
     _case("bf16", 1, 2, 2, 150, 150, 64, sm_scale=1.0), _case("f32", 1, 2, 2, 100, 100, 64, sm_scale=1.0),
+    # many tiles: eight waves a tile (128 to 256 tiles of 128 rows, causal to 512), four waves a tile beyond that
+    *[_case("bf16", 4, 16, 16, 200, 200, d, causal=c) for d in (16, 32, 64, 128) for c in (False, True)], *[_case("f32", 4, 16, 16, 200, 200, d, causal=True) for d in (16, 32, 64, 128)],
+    *[_case("bf16", 10, 13, 13, 270, 300, d) for d in (16, 32, 64, 128)], *[_case("bf16", 12, 16, 16, 290, 270, d, causal=True) for d in (32, 64, 128)],
+    *[_case("f32", 10, 13, 13, 140, 300, d) for d in (16, 32, 64, 128)], _case("bf16", 6, 48, 12, 150, 129, 128, causal=True, layout="tokens"), _case("bf16", 6, 48, 12, 150, 129, 64, layout="piece"),
+    _case("bf16", 12, 32, 16, 140, 260, 64, causal=True, lens=([140, 3, 0, 77, 128, 129, 140, 1, 64, 65, 100, 139], [260, 3, 5, 0, 256, 257, 70, 260, 64, 33, 100, 1])),
+    # and their other axis cut
+    _case("bf16", 2, 15, 15, 200, 4200, 128), _case("bf16", 2, 15, 15, 4200, 200, 64), _case("bf16", 2, 30, 15, 100, 6400, 64, causal=True), _case("f32", 2, 15, 15, 200, 4100, 128), _case("f32", 2, 15, 15, 4100, 200, 128),
+    # few rows and many keys: the row tiles narrow, the key tiles not
+    *[_case("bf16", 1, 4, 4, 1, 5000, d) for d in (32, 64, 128)], _case("bf16", 1, 16, 16, 20, 1100, 64, causal=True), _case("bf16", 10, 16, 16, 33, 130, 128), _case("f32", 1, 16, 16, 20, 1100, 16, causal=True),
+    _case("bf16", 8, 32, 32, 30, 300, 64, lens=([30, 1, 0, 15, 30, 30, 29, 2], [300, 300, 300, 0, 129, 128, 1, 64])),
     # the kernels of one wave a row
     _case("bf16", 2, 4, 2, 40, 50, 64, causal=True, lens=([40, 17], [50, 9]), path=1), _case("f32", 1, 2, 1, 33, 20, 128, path=1), _case("bf16", 1, 2, 1, 20, 33, 16, causal=True, path=1),
 ]
@@ -130,34 +140,72 @@ def test_dense_against_64_bits(c):
     _check(c, _run(c, *x), *x)
 
 
-@pytest.mark.parametrize("path", [0, 1])
-@pytest.mark.parametrize("dtype,d,bad", [("bf16", 64, math.nan), ("bf16", 128, math.inf), ("f32", 32, -math.inf), ("bf16", 16, math.nan)])
-def test_nothing_behind_a_mask_is_seen(dtype, d, bad, path):
-    """Infinities and NaN behind the lengths and in keys and queries that a causal mask hides: what is not masked is as if they were zeros."""
-    c = _case(dtype, 2, 4, 2, 100, 100, d, causal=True, lens=([100, 40], [100, 40]), path=path)
+MASKED = [("bf16", 64, math.nan, 2, 2, 100, 0), ("bf16", 128, math.inf, 2, 2, 100, 0), ("f32", 32, -math.inf, 2, 2, 100, 0), ("bf16", 16, math.nan, 2, 2, 100, 0),
+          ("bf16", 64, math.nan, 2, 2, 100, 1), ("f32", 128, math.inf, 2, 2, 100, 1), ("bf16", 128, math.nan, 2, 16, 520, 0), ("bf16", 64, math.inf, 2, 64, 520, 0), ("f32", 128, math.nan, 2, 16, 520, 0),
+          ("bf16", 64, math.nan, 2, 1, 1800, 0), ("bf16", 128, math.inf, 2, 1, 1800, 0)]
+
+
+@pytest.mark.parametrize("dtype,d,bad,batch,kv_heads,N,path", MASKED, ids=str)
+def test_nothing_behind_a_mask_is_seen(dtype, d, bad, batch, kv_heads, N, path):
+    """Infinities and NaN behind the lengths and in keys and queries that a causal mask hides: what is not masked is as if they were zeros.  One tile a
+    group, many, and few with the other axis cut."""
+    short = N * 2 // 5
+    c = _case(dtype, batch, 2 * kv_heads, kv_heads, N, N, d, causal=True, lens=([N, short], [N, short]), path=path)
     Q, K, V, dO, ql, kl = _inputs(c)
     clean = [t.clone() for t in (Q, K, V, dO)]
     for t in (Q, K, V, dO):
-        t[1, :, 40:] = bad                          # behind the lengths
+        t[1, :, short:] = bad                       # behind the lengths
     K[0, 0, 71], V[0, 0, 71, 3] = bad, bad         # seen by queries 71 and on
     got = _run(c, Q, K, V, dO, ql, kl)
     want = _run(c, *clean, ql, kl)
+    near = lambda g, w: torch.isfinite(g).all() and float((g - w).abs().max()) <= 2.0 ** -6 * float(w.abs().max())      # another kernel's rounding: a few of P's and the result's half steps
     for n in ("O", "LSE", "dQ"):
         assert torch.equal(got[n][1], want[n][1]) and torch.equal(got[n][0, 2:], want[n][0, 2:]), n
-        g, w = got[n][0, :2, :71].double(), want[n][0, :2, :71].double()
-        assert torch.isfinite(g).all()
-        assert float((g - w).abs().max()) <= 2.0 ** -6 * float(w.abs().max()), n      # another kernel's rounding: a few of P's and the result's half steps
+        assert near(got[n][0, :2, :71].double(), want[n][0, :2, :71].double()), n
     for n in ("dK", "dV"):
-        assert torch.equal(got[n][1], want[n][1]) and torch.equal(got[n][0, 1], want[n][0, 1]), n
+        assert torch.equal(got[n][1], want[n][1]) and torch.equal(got[n][0, 1:], want[n][0, 1:]), n
     # a query and its gradient that hold a NaN: keys behind it do not see it
     Q, K, V, dO = clean
     Q[0, 1, 20, 1], dO[0, 1, 30, 2] = bad, bad
     got2 = _run(c, Q, K, V, dO, ql, kl)
-    keep = [i for i in range(100) if i != 20]
-    assert torch.isfinite(got2["O"][0, 1, keep].float()).all() and torch.equal(got2["O"][0, [0, 2, 3]], want["O"][0, [0, 2, 3]])
+    keep = [i for i in range(N) if i != 20]
+    others = [h for h in range(2 * kv_heads) if h != 1]
+    assert torch.isfinite(got2["O"][0, 1, keep].float()).all() and torch.equal(got2["O"][0, others], want["O"][0, others])
     for n in ("dK", "dV"):
-        g, w = got2[n][0, 0, 31:].double(), want[n][0, 0, 31:].double()
-        assert torch.isfinite(g).all() and float((g - w).abs().max()) <= 2.0 ** -6 * float(w.abs().max()), n
+        assert near(got2[n][0, 0, 31:].double(), want[n][0, 0, 31:].double()), n
+
+
+@pytest.mark.parametrize("dtype,d,heads,N", [("bf16", 64, 2, 130), ("f32", 64, 2, 130), ("bf16", 128, 64, 200), ("bf16", 64, 64, 600), ("bf16", 32, 1, 3000)], ids=str)
+def test_nothing_behind_the_lengths_is_seen_without_a_causal_mask(dtype, d, heads, N):
+    c = _case(dtype, 2, heads, heads, N, N, d, lens=([N, N // 3], [N - 1, N // 3 + 1]))
+    Q, K, V, dO, ql, kl = _inputs(c)
+    want = _run(c, Q.clone(), K.clone(), V.clone(), dO.clone(), ql, kl)
+    for b in range(2):
+        for t, n in ((Q, ql), (K, kl), (V, kl), (dO, ql)):
+            t[b, :, int(n[b]):] = math.nan
+    got = _run(c, Q, K, V, dO, ql, kl)
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+
+
+def test_two_problems_at_once_on_two_streams():
+    """A plan, a workspace and a stream each, enqueued in turn and waited for once."""
+    jobs = []
+    for c in (_case("bf16", 2, 8, 4, 500, 900, 64, causal=True), _case("bf16", 1, 4, 4, 1, 5000, 128)):
+        x = _inputs(c)
+        p = _plan(c, *x[:3])
+        want = _run(c, *x)
+        jobs.append((p, x, p.alloc_workspace(True), torch.cuda.Stream(), want, []))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, (Q, K, V, dO, _, _), ws, stream, _, out in jobs:
+            with torch.cuda.stream(stream):
+                O, LSE = llsa.dense_forward(p, Q, K, V, workspace=ws)
+                out.append((O, LSE, *llsa.dense_backward(p, Q, K, V, O, LSE, dO, workspace=ws)))
+    torch.cuda.synchronize()
+    for *_, want, out in jobs:
+        for o in out:
+            assert all(torch.equal(a, want[n]) for a, n in zip(o, ("O", "LSE", "dQ", "dK", "dV")))
 
 
 def test_dense_is_the_same_bits_from_call_to_call_and_stream_to_stream():
