@@ -121,21 +121,26 @@ template <class T, int D> __global__ void __launch_bounds__(256) glue_bwd_kernel
     }
 }
 
-// The workgroups' sums added up: 64 slices of 16 columns a workgroup, each slice every 64th workgroup's, then the slices in order.
+// The workgroups' sums added up: 128 slices of 8 columns a workgroup, each slice every 128th workgroup's, then the slices in order.
 template <int D> __global__ void __launch_bounds__(1024) glue_sums_kernel(GlueBwdArgs a) {
-    __shared__ float lds[64][17];
-    const int col = threadIdx.x & 15, c = blockIdx.x * 16 + col, slice = threadIdx.x >> 4;
+    __shared__ float lds[128][9];
+    const int col = threadIdx.x & 7, c = blockIdx.x * 8 + col, slice = threadIdx.x >> 3;
     float s = 0.f;
-#pragma unroll 8
-    for (int w = slice; w < a.wgs; w += 64) s += a.part[(int64_t)w * 2 * D + c];
+    for (int w0 = slice; w0 < a.wgs; w0 += 1024) {           // eight on their way at once
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = a.part[(int64_t)min(w0 + 128 * j, a.wgs - 1) * 2 * D + c];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += w0 + 128 * j < a.wgs ? v[j] : 0.f;
+    }
     lds[slice][col] = s;
     __syncthreads();
-    if (slice < 4) {                                         // 16 slices each, then those four
+    if (slice < 8) {                                         // 16 slices each, then those eight
         s = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s += lds[slice * 16 + i][col];
-        s += __shfl_xor(s, 16, 64);
-        s += __shfl_xor(s, 32, 64);
+#pragma unroll
+        for (int o = 8; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
         if (slice == 0) a.dgamma[c / D][c % D] = s;
     }
 }
@@ -178,7 +183,7 @@ hipError_t launch_glue_backward(const Plan &p, const void *Qpre, const void *Kpr
         else            glue_bwd_kernel<__bf16, D><<<dim3(gx, gy), 256, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        glue_sums_kernel<D><<<2 * D / 16, 1024, 0, s>>>(a);
+        glue_sums_kernel<D><<<2 * D / 8, 1024, 0, s>>>(a);
         return hipGetLastError();
     };
     switch (p.d) {

@@ -366,72 +366,56 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_bwd_kernel(NormArgs a)
     }
 }
 
-// The workgroups' sums added up: 64 slices of 16 channels a workgroup, each slice every 64th workgroup's, then the slices in order.
+// The workgroups' sums added up, E, T and F each by workgroups of their own: 64 slices of 16 channels a workgroup, each slice every 64th workgroup's, then the slices in order.
 __global__ void __launch_bounds__(1024) norm_sums_kernel(NormArgs a) {
-    __shared__ float lds[3][64][17];
-    const int col = threadIdx.x & 15, c = blockIdx.x * 16 + col, slice = threadIdx.x >> 4;
+    __shared__ float lds[64][17];
+    const int which = blockIdx.y, col = threadIdx.x & 15, c = blockIdx.x * 16 + col, slice = threadIdx.x >> 4;
+    float *const per_batch = which == 0 ? a.dscale : which == 1 ? a.dshift : a.dgate, *const per_channel = which == 0 ? a.dgain : which == 1 ? nullptr : a.dgain_branch;
+    if (!per_batch && !per_channel) return;
     const bool in = c < a.C;
-    float dgain = 0.f, dgb = 0.f, shared[3] = {0.f, 0.f, 0.f};
-    const float gain = in && a.gain ? a.gain[c] : 1.f, gb = in && a.gain_branch ? a.gain_branch[c] : 1.f;
+    const float *of = which == 0 ? a.gain : which == 1 ? nullptr : a.gain_branch;      // what a batch entry's gradient is multiplied by; the channel's: by its modulation
+    const float f = (which == 2 ? a.alpha : 1.f) * (in && of ? of[c] : 1.f);
+    float all = 0.f, shared = 0.f;
     for (int b0 = 0; b0 < a.batch; b0 += 2) {                // two batch entries' and eight workgroups' sums on their way at once
-        float s[2][3] = {};
+        float s[2] = {0.f, 0.f};
         if (in) {
             for (int w0 = slice; w0 < a.blocks; w0 += 512) {
-                float v[8][2][3];
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float *p = a.part + ((int64_t)min(b0 + i, a.batch - 1) * a.blocks + min(w0 + 64 * j, a.blocks - 1)) * 3 * a.C + c;
-#pragma unroll
-                        for (int k = 0; k < 3; ++k) v[j][i][k] = p[k * a.C];
-                    }
+                float v[8][2];
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
+                        v[j][i] = a.part[(((int64_t)min(b0 + i, a.batch - 1) * a.blocks + min(w0 + 64 * j, a.blocks - 1)) * 3 + which) * a.C + c];
 #pragma unroll
-                        for (int k = 0; k < 3; ++k) s[i][k] += w0 + 64 * j < a.blocks ? v[j][i][k] : 0.f;
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) s[i] += w0 + 64 * j < a.blocks ? v[j][i] : 0.f;
             }
         }
         for (int i = 0; i < 2 && b0 + i < a.batch; ++i) {
             const int b = b0 + i;
-#pragma unroll
-            for (int k = 0; k < 3; ++k) lds[k][slice][col] = i == 0 ? s[0][k] : s[1][k];
+            lds[slice][col] = i == 0 ? s[0] : s[1];
             __syncthreads();
             if (slice < 4) {                                 // 16 slices each, then those four
-                float v[3];
+                float v = 0.f;
 #pragma unroll
-                for (int k = 0; k < 3; ++k) {
-                    v[k] = 0.f;
-#pragma unroll
-                    for (int q = 0; q < 16; ++q) v[k] += lds[k][slice * 16 + q][col];
-                    v[k] += __shfl_xor(v[k], 16, 64);
-                    v[k] += __shfl_xor(v[k], 32, 64);
-                }
+                for (int q = 0; q < 16; ++q) v += lds[slice * 16 + q][col];
+                v += __shfl_xor(v, 16, 64);
+                v += __shfl_xor(v, 32, 64);
                 if (slice == 0 && in) {
                     const int64_t at = b * a.mod_stride + c;
-                    dgain = fmaf(1.f + n_mod(a.scale, a.mod_f32, at, 0.f), v[0], dgain);
-                    dgb = fmaf(a.alpha * n_mod(a.gate, a.mod_f32, at, 1.f), v[2], dgb);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) shared[k] += v[k];
+                    all = fmaf(which == 0 ? 1.f + n_mod(a.scale, a.mod_f32, at, 0.f) : a.alpha * n_mod(a.gate, a.mod_f32, at, 1.f), v, all);
+                    shared += v;
                     if (a.mod_stride || b == a.batch - 1) {
-                        const int64_t to = (a.mod_stride ? (int64_t)b * a.C : 0) + c;
-                        if (a.dscale) a.dscale[to] = gain * shared[0];
-                        if (a.dshift) a.dshift[to] = shared[1];
-                        if (a.dgate) a.dgate[to] = a.alpha * gb * shared[2];
-#pragma unroll
-                        for (int k = 0; k < 3; ++k) shared[k] = 0.f;
+                        if (per_batch) per_batch[(a.mod_stride ? (int64_t)b * a.C : 0) + c] = f * shared;
+                        shared = 0.f;
                     }
                 }
             }
             __syncthreads();
         }
     }
-    if (slice == 0 && in) {
-        if (a.dgain) a.dgain[c] = dgain;
-        if (a.dgain_branch) a.dgain_branch[c] = dgb;
-    }
+    if (slice == 0 && in && per_channel) per_channel[c] = all;
 }
 
 // The fewest threads a row that hold it with at most `most` channels each, 4 to 64 or whole waves.
@@ -505,7 +489,7 @@ hipError_t launch_norm_backward(const NormPlan &p, NormArgs a, hipStream_t s) {
     });
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
-    norm_sums_kernel<<<(a.C + 15) / 16, 1024, 0, s>>>(a);
+    norm_sums_kernel<<<dim3((a.C + 15) / 16, 3), 1024, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -119,6 +119,25 @@ def test_norm_in_place_and_without_a_next_block():
     assert torch.equal(c, x_out) and torch.equal(y2, y)
 
 
+@pytest.mark.parametrize("layer", [False, True], ids=["rms", "layer"])
+@pytest.mark.parametrize("shape,dtype", [((2, 9, 5), torch.bfloat16), ((2, 9, 511), torch.float32), ((1, 700, 1023), torch.bfloat16), ((2, 1100, 2050), torch.bfloat16), ((1, 2, 8189), torch.float32)], ids=str)
+def test_norm_in_place_over_every_row_length(shape, dtype, layer):
+    """Rows that several waves share, whose last vectors overlap, and that one thread has alone; a workspace that holds NaN."""
+    p, t, dy, dx_out, x_out, stats, grads = _run(shape, dtype, torch.float32, layer, PARTS[0], False, False)
+    rest = {k: v for k, v in t.items() if k not in ("x", "branch")}
+    x, br = t["x"].clone(), t["branch"].clone()
+    assert torch.equal(llsa.norm_forward(p, x, br, **rest, x_out=x)[0], x_out)
+    x = t["x"].clone()
+    assert torch.equal(llsa.norm_forward(p, x, br, **rest, x_out=br)[0], x_out)
+    args = [t[n] for n in ("gain_branch", "gate", "gain", "scale", "shift")]
+    ws = p.alloc_workspace()
+    for into in ("dy", "dx_out"):
+        g, r, br = dy.clone(), dx_out.clone(), t["branch"].clone()
+        ws.fill_(0xff)
+        got = llsa.norm_backward(p, x_out, g, stats, br, *args, dx_out=r, dx=g if into == "dy" else r, dbranch=br, workspace=ws)
+        assert all(torch.equal(got[n], grads[n]) for n in grads), into
+
+
 def test_a_row_that_is_not_finite_stays_alone():
     p, t, dy, dx_out, x_out, stats, grads = _run((2, 40, 136), torch.bfloat16, torch.bfloat16, True, PARTS[0], False, False)
     t["x"][0, 7, 3], t["branch"][1, 0, 135] = math.nan, math.inf
@@ -297,6 +316,7 @@ def test_a_block_of_all_of_them_against_automatic_differentiation():
         dy1 += flat(g) @ par[n].T
     b1 = llsa.norm_backward(n1, par["x"], dy1, st1, gain=par["gain"], scale=par["scale"], shift=par["shift"], dx_out=b2["dx"])
     got["x"], got["gain"], got["scale"], got["shift"] = b1["dx"], b1["dgain"], b1["dscale"], b1["dshift"]
+    out = out.detach()
     assert float((got_out.double() - out).abs().max()) <= 1e-4 * float(out.abs().max())
     assert set(got) == set(par)
     for n in par:
