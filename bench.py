@@ -280,7 +280,7 @@ def main():
     ap.add_argument("--stage", default="auto", help="stage whose kernel is bracketed by HIP events in the timed region")
     ap.add_argument("--no-cpu", action="store_true", help="skip the CPU-oracle leg")
     ap.add_argument("--all-stages", action="store_true", help="after the timed region, one more pass timing every stage")
-    ap.add_argument("--dense-compare", action="store_true", help="also time dense bf16 SDPA (forward) on this GPU")
+    ap.add_argument("--dense-compare", action="store_true", help="also time dense attention on this GPU: the library's forward and backward, and torch's SDPA (forward)")
     ap.add_argument("--force-generic", action="store_true", help="run the fp32-arithmetic kernels that take any shape")
     ap.add_argument("--no-graph", action="store_true", help="time eager launches instead of HIP-graph replays of the step")
     ap.add_argument("--order", default="raster", choices=["raster", "nested"],
@@ -345,10 +345,11 @@ def main():
         bhNd = cfg["batch"] * cfg["heads"] * cfg["N"] * cfg["d"]
         cos, sin = (torch.from_numpy(a).cuda() for a in inputs.rope_tables(cfg["N"], cfg["d"]))
         gq, gk = (torch.from_numpy(inputs.norm_gain(1, w, cfg["d"])).cuda() for w in ("Q", "K"))
-        ws2 = case.plan.alloc_workspace(False)
+        ws2, gws = case.plan.alloc_workspace(False), case.plan.alloc_glue_workspace()
         res = {}
         for name, fn in (("qknorm_rope_pool", lambda: llsa.qknorm_rope_pool(case.plan, case.Q, case.K, case.V, gq, gk, cos, sin, 1e-6, ws2)),
-                         ("pool", lambda: llsa.pool(case.plan, case.Q, case.K, case.V, case.ws))):
+                         ("pool", lambda: llsa.pool(case.plan, case.Q, case.K, case.V, case.ws)),
+                         ("qknorm_rope_backward", lambda: llsa.qknorm_rope_backward(case.plan, case.Q, case.K, gq, gk, cos, sin, case.dO, case.V, 1e-6, workspace=gws))):
             for _ in range(3):
                 fn()
             med, mn = step_events(fn, args.steps)
@@ -359,6 +360,8 @@ def main():
         res["qknorm_rope_pool"]["gbps_at_median"] = glue_bytes / res["qknorm_rope_pool"]["median_ms"] / 1e6
         res["pool"]["algorithmic_bytes"] = pool_bytes
         res["pool"]["gbps_at_median"] = pool_bytes / res["pool"]["median_ms"] / 1e6
+        res["qknorm_rope_backward"]["algorithmic_bytes"] = 6.0 * bhNd * elt    # Q, K and their gradients read, two gradients written
+        res["qknorm_rope_backward"]["gbps_at_median"] = 6.0 * bhNd * elt / res["qknorm_rope_backward"]["median_ms"] / 1e6
         res["unfused_estimate_bytes"] = pool_bytes + 4.0 * bhNd * elt   # a separate glue kernel reads and writes Q and K
         print(json.dumps({"glue": res, "workload": cfg["name"]}))
         return
@@ -499,6 +502,20 @@ def main():
             F.scaled_dot_product_attention(case.Q, case.K, case.V)
         torch.cuda.synchronize()
         out["dense_sdpa_fwd_ms"] = (time.perf_counter() - t0) / 3 * 1e3
+        dense = llsa.DensePlan(cfg["batch"], cfg["heads"], cfg["N"], cfg["N"], cfg["d"], dtype=case.plan.desc.dtype)
+        dws = dense.alloc_workspace(True)
+        for name, call in (("fwd", lambda: llsa.dense_forward(dense, case.Q, case.K, case.V, workspace=dws)),
+                           ("bwd", lambda: llsa.dense_backward(dense, case.Q, case.K, case.V, Od, LSEd, case.dO, workspace=dws))):
+            for _ in range(2):
+                got = call()
+            torch.cuda.synchronize()
+            t0 = time.perf_counter()
+            for _ in range(3):
+                got = call()
+            torch.cuda.synchronize()
+            out[f"dense_llsa_{name}_ms"] = (time.perf_counter() - t0) / 3 * 1e3
+            if name == "fwd":
+                Od, LSEd = got
 
     if not args.no_cpu:
         threads = min(16, os.cpu_count() or 1, cfg["batch"] * cfg["heads"])

@@ -2,6 +2,10 @@
 // tiles of KT through LDS, the running maximum and sum of a softmax in registers.  A lane has one row: its scores come out of the first product in the
 // registers that the second one takes, O^T = V^T P^T collects channels in the registers of the same lane, so maximum, sum and rescaling are
 // the lane's own (and its partner's in the other half of the wave).
+//
+// 4 d operations a pair of a query and a key: 16 heads x 16384 tokens, d = 64, 1115 to 1190 us (960 TFLOP/s), where the softmax (an exponential a pair and some five other vector instructions) takes the
+// issue slots that the matrix unit does not; 4 heads x 32768, d = 128, 1.94 ms (1130 TFLOP/s; a large library product reaches 1336, clocks under that load included).  One token of 32 heads over 8 key
+// heads, 8 sequences of 500 to 16384, d = 128: 60 us and 6 for the join, 5.0 TB/s of the keys that are there.
 #include "dense_row.h"
 #include "dense_tile.h"
 

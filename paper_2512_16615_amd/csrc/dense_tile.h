@@ -177,7 +177,7 @@ __device__ __forceinline__ void buffer_to_lds_dword(u32x4 buf, unsigned v, unsig
 #pragma clang diagnostic pop
 
 // Every load that the compiler knows of is done.  In front of a loop that waits for its ring by itself: the compiler would wait inside it, in each
-// round, for what the first one uses, and so for the ring's newest tile (causal, 3 x 16 heads x 1999 tokens, d = 128: forward 59 -> 40 us).
+// round, for what the first one uses, and so for the ring's newest tile (causal, 3 x 16 heads of 1999, 1500 and 700 tokens, d = 128: forward 59.5 -> 53.3 us).
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 // A wave's share of a tile of ROWS rows: loads first, first + 1, .. of it (1024 bytes each).

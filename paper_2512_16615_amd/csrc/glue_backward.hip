@@ -2,7 +2,8 @@
 //   dy[2i] = g[2i] cos + g[2i+1] sin, dy[2i+1] = g[2i+1] cos - g[2i] sin        (the rotation's transpose; g: gradient of Xout)
 //   dgamma += dy x^;   p = dy gamma;   dx = r (p - x^ mean(p x^))
 // A thread has 16 bytes of channels of one token and walks over the heads, Q and K in turn, so that a token's cosines and sines are read once for
-// all of them; the d / (16 / element size) threads of a row are neighbouring lanes.  Bytes bound it: three tensors' worth of memory for each of Q and K.
+// all of them; the d / (16 / element size) threads of a row are neighbouring lanes.  Bytes bound it, three tensors' worth for each of Q and K:
+// 16 heads x 65536 tokens, d = 64, bf16, 153 us (822 MB, 5.4 TB/s) and 5 for the sums; 16 x 4096 12 and 2.7.
 // dgamma: a thread's sums over its heads, then over the workgroup's tokens, to the workspace; a second launch adds the workgroups in a fixed order.
 #include <algorithm>
 #include <type_traits>

@@ -673,8 +673,8 @@ const char *llsa_status_string(llsa_status s) {
     switch (s) {
         case LLSA_OK: return "ok";
         case LLSA_ERR_NULL: return "null pointer";
-        case LLSA_ERR_BAD_SHAPE: return "bad shape (N must be divisible by B^L; L >= 1; 0 <= Le <= L; K >= 1)";
-        case LLSA_ERR_UNSUPPORTED: return "unsupported d / B / K / dtype / size";
+        case LLSA_ERR_BAD_SHAPE: return "bad shape, stride or alignment (of a sparse layer: N must be divisible by B^L; L >= 1; 0 <= Le <= L; K >= 1)";
+        case LLSA_ERR_UNSUPPORTED: return "unsupported d / B / K / C / dtype / kind / size";
         case LLSA_ERR_WORKSPACE: return "the problem's forward workspace exceeds the library's static one";
         case LLSA_ERR_RUNTIME: return "HIP launch failed";
     }

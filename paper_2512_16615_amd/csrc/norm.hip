@@ -7,6 +7,8 @@
 // and per channel and batch entry three sums over the rows: E = sum dy h^, T = sum dy, F = sum dh u, from which
 //   dgain = sum_b (1 + scale) E, dscale = gain E, dshift = T, dgate = alpha gain_branch F, dgain_branch = alpha sum_b gate F.
 // A thread keeps its channels' sums over all its rows; the workgroups' sums go to the workspace and a second launch adds them in a fixed order.
+// Bytes bound it: 2 x 16384 rows of 1024 in bf16, forward 45 us (268 MB, 5.9 TB/s: part of it still in the last cache level), backward 82 to 90 (403 MB, 4.7 TB/s) and 7.6 for the sums; 3 x 2704 rows of
+// 1001 in fp32 with LayerNorm, whose rows begin at any element, backward 35 us (5.5 TB/s) and 9.
 #include "norm.h"
 
 #include <new>
@@ -245,7 +247,7 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_bwd_kernel(NormArgs a)
 #pragma unroll
     for (int i = 0; i < E; ++i) sE[i] = sT[i] = sF[i] = 0.f;
     // The next row is on its way while this one is worked on (32768 rows of 1024: 93 -> 83 us), but where a thousand threads leave no registers
-    // for it. 
+    // for it.
     constexpr bool AHEAD = TPR < 1024;
     const int64_t step = (int64_t)gridDim.x * GP;
     int64_t n = (int64_t)blockIdx.x * GP + threadIdx.x / TPR;

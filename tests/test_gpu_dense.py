@@ -276,6 +276,27 @@ def test_dense_reads_broadcast_keys_and_offsets_beyond_32_bits():
     del store, K, V
 
 
+@pytest.mark.parametrize("heads,kv_heads,causal,d", [(16, 16, False, 64), (8, 4, True, 128), (1, 1, False, 32)], ids=str)
+def test_dense_step_on_tensors_beyond_32_bits(heads, kv_heads, causal, d):
+    """Everything 2 MB from token to token, read and written more than 4 GB behind its first element: the same bits as contiguous."""
+    n, step = 2200, 1 << 20
+    c = _case("bf16", 1, heads, kv_heads, n, n, d, causal=causal)
+    Q, K, V, dO, _, _ = _inputs(c)
+    want = _run(c, Q, K, V, dO, None, None)
+    stores = [torch.empty(n * step, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    far = lambda store, i, h: store.as_strided((1, h, n, d), (n * step, d, step, 1), i * heads * d)
+    x = [far(stores[0], i, t.shape[1]) for i, t in enumerate((Q, K, V, dO))]
+    for t, s in zip(x, (Q, K, V, dO)):
+        t.copy_(s)
+    p = _plan(c, *x[:3])
+    O, dQ, dK, dV = (far(stores[1], i, h) for i, h in enumerate((heads, heads, kv_heads, kv_heads)))
+    _, LSE = llsa.dense_forward(p, *x[:3], O=O)
+    llsa.dense_backward(p, *x[:3], O, LSE, x[3], dQ=dQ, dK=dK, dV=dV)
+    for t, w in ((O, "O"), (LSE, "LSE"), (dQ, "dQ"), (dK, "dK"), (dV, "dV")):
+        assert torch.equal(t, want[w]), w
+    del stores, x
+
+
 def test_dense_binding_refuses_what_does_not_fit():
     c = _case("bf16", 2, 2, 2, 40, 40, 64)
     Q, K, V, dO, _, _ = _inputs(c)

@@ -33,6 +33,10 @@ def test_layouts_match_the_header(llsa):  # noqa: F811
     (dict(k_stride=(-64, 64, 64)), 2),
     (dict(o_stride=(0, 64, 512)), 2),           # batch entries of O on top of each other
     (dict(o_stride=(1 << 20, 64, 256)), 2),     # heads 4 .. 7 of a token are heads 0 .. 3 of the next
+    (dict(batch=1, heads=60000, Nq=1 << 20), 3),                             # more tiles than a launch takes
+    (dict(batch=1, heads=64, kv_heads=1, Nq=1 << 25), 3),
+    (dict(k_stride=(1 << 33, 1 << 32, 1 << 23)), 3),                         # 256 tokens 4 GiB apart
+    (dict(q_stride=(1 << 34, 1 << 31, 64), kv_heads=4), 3),                  # two heads of a key head 4 GiB apart
 ])
 def test_dense_plan_refuses(llsa, kw, status):  # noqa: F811
     args = dict(batch=2, heads=8, Nq=128, Nkv=128, d=64)
@@ -46,6 +50,8 @@ def test_dense_plan_takes_layouts_of_projections(llsa):  # noqa: F811
     s = (128 * 3 * 8 * 64, 64, 3 * 8 * 64)      # a piece of a projection to queries, keys and values
     llsa.DensePlan(2, 8, 128, 128, 64, q_stride=s, k_stride=s, v_stride=s, o_stride=(128 * 8 * 64, 64, 8 * 64))
     llsa.DensePlan(2, 8, 128, 128, 64, k_stride=(0, 0, 64), v_stride=(0, 0, 64))
+    llsa.DensePlan(2, 8, 128, 128, 64, k_stride=(1 << 33, 1 << 32, 1 << 23), kernel_path=1)
+    llsa.DensePlan(2, 8, 128, 128, 64, q_stride=(1 << 34, 1 << 31, 64))     # heads with keys of their own are any distance apart
     llsa.DensePlan(1, 1, 1, 1, 16, q_stride=(3, 5, 7))                      # strides that nobody takes a step with
 
 
