@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "lanes.h"
 #include "llsa_internal.h"
 
 namespace llsa {
@@ -94,11 +95,8 @@ template <class T, int D> __global__ void __launch_bounds__(256) glue_bwd_kernel
                 ss = fmaf(x[e], x[e], ss);
                 px = fmaf(dy[e] * gam[y][e], x[e], px);
             }
-#pragma unroll
-            for (int o = 1; o < VPR; o <<= 1) {
-                ss += __shfl_xor(ss, o, 64);
-                px += __shfl_xor(px, o, 64);
-            }
+            ss = lanes_sum<VPR>(ss);
+            px = lanes_sum<VPR>(px);
             const float r = 1.f / sqrtf(fmaf(ss, a.inv_d, a.eps)), m = px * r * a.inv_d;
 #pragma unroll
             for (int e = 0; e < VN; ++e) {

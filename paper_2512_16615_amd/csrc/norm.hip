@@ -1,5 +1,5 @@
-// The norms between two blocks with gate and residual, forward and backward: one pass over the rows, each held in registers by 16 to 1024
-// threads (at most 16 channels a thread forward, 8 backward), so that a row is read once and written once.  What varies by channel only (the gains, and the
+// The norms between two blocks with gate and residual, forward and backward: one pass over the rows, each held in registers by 16 to 512
+// threads (at most 16 channels a thread), so that a row is read once and written once.  What varies by channel only (the gains, and the
 // modulation of the batch entry that a workgroup belongs to) stays in registers over all rows of the workgroup, combined:
 //   y = n(x') ga + sh, x' = x + gz n(branch)       with ga = gain (1 + scale), sh = shift, gz = alpha gate gain_branch.
 // Backward, per row, with h^ = n(x'), u = n(branch) (or the branch itself):
@@ -7,10 +7,12 @@
 // and per channel and batch entry three sums over the rows: E = sum dy h^, T = sum dy, F = sum dh u, from which
 //   dgain = sum_b (1 + scale) E, dscale = gain E, dshift = T, dgate = alpha gain_branch F, dgain_branch = alpha sum_b gate F.
 // A thread keeps its channels' sums over all its rows; the workgroups' sums go to the workspace and a second launch adds them in a fixed order.
-// Bytes bound it: 2 x 16384 rows of 1024 in bf16, forward 45 us (268 MB, 5.9 TB/s: part of it still in the last cache level), backward 82 to 90 (403 MB, 4.7 TB/s) and 7.6 for the sums; 3 x 2704 rows of
-// 1001 in fp32 with LayerNorm, whose rows begin at any element, backward 35 us (5.5 TB/s) and 9.
+// Bytes bound it, cold: 2 x 16384 rows of 1024 in bf16, forward 52 us (268 MB, 5.15 TB/s), backward 84 (403 MB, 4.8 TB/s) and 7.6 for the sums; 3 x 2704 rows of 1001 in fp32 with LayerNorm, whose
+// rows begin at any element, backward 54 in all (195 MB, 3.6 TB/s).
+#include "lanes.h"
 #include "norm.h"
 
+#include <algorithm>
 #include <new>
 #include <type_traits>
 
@@ -38,27 +40,31 @@ template <class T> __device__ __forceinline__ void n_unpack(const typename NVec<
         }
     }
 }
-// Which channels of a row a thread has: NV vectors of n, number k at channel (k TPR + t) n.  FULL: the vectors cover the row exactly.  Otherwise
-// the last one that is not whole is read n channels from the row's end (so that no load needs a branch) and only its last ones are the
-// thread's own; one beyond the row has none.  What is not its own counts as zeros and is not written.
-template <class T, int TPR, int NV, bool FULL> struct Channels {
+// Which channels of a row a thread has: NV vectors of n, number k at channel (k TPR + t) n.  The form is a row's:
+//   kWhole: the vectors cover it exactly
+//   kTail: the last one that is not whole is read n channels from the row's end, and only its last ones are the thread's own; one beyond the row is read at its beginning
+//          and has none.  No load needs a branch.
+//   kShort: fewer than n channels, element by element
+enum NormRow { kWhole, kTail, kShort };
+template <class T, int TPR, int NV, int ROW> struct Channels {
     static constexpr int n = NVec<T>::n, E = NV * n;
+    static constexpr bool whole = ROW == kWhole, vectors = ROW != kShort;
     int first[NV], own[NV], C;                               // where a vector is read, its first element that is the thread's own
     __device__ __forceinline__ Channels(int t, int C_) : C(C_) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = (k * TPR + t) * n;
-            first[k] = FULL || c + n <= C ? c : c < C ? max(0, C - n) : 0;
-            own[k] = FULL || c + n <= C ? 0 : c < C ? c - first[k] : n;
+            first[k] = whole || (c + n <= C || !vectors) ? c : c < C ? C - n : 0;
+            own[k] = whole || c + n <= C || (!vectors && c < C) ? 0 : c < C ? c - first[k] : n;
         }
     }
     __device__ __forceinline__ int channel(int i) const { return first[i / n] + i % n; }
-    __device__ __forceinline__ bool mine(int i) const { return FULL || (i % n >= own[i / n] && channel(i) < C); }
-    // a row's channels as they stand in memory (an element's 16 bits or 32 a register where the row has no whole vector), and as numbers
+    __device__ __forceinline__ bool mine(int i) const { return whole || (i % n >= own[i / n] && (vectors || channel(i) < C)); }
+    // a row's channels as they stand in memory, and as numbers; what is not the thread's own is some other channel of the row (kShort: 0)
     struct Raw { typename NVec<T>::Raw r[NV]; };
     __device__ __forceinline__ void ask(const char *base, int64_t at, Raw &x) const {
         const T *row = reinterpret_cast<const T *>(base) + at;
-        if (FULL || C >= n) {
+        if constexpr (vectors) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) x.r[k] = *reinterpret_cast<const typename NVec<T>::Raw *>(row + first[k]);
         } else {
@@ -71,19 +77,20 @@ template <class T, int TPR, int NV, bool FULL> struct Channels {
     __device__ __forceinline__ void get(const Raw &r, float (&x)[E]) const {
 #pragma unroll
         for (int k = 0; k < NV; ++k) n_unpack<T>(r.r[k], x + k * n);
-#pragma unroll
-        for (int i = 0; !FULL && i < E; ++i) x[i] = mine(i) ? x[i] : 0.f;
     }
+    // .. with zeros for what is not the thread's own
     __device__ __forceinline__ void load(const char *base, int64_t at, float (&x)[E]) const {
         Raw r;
         ask(base, at, r);
         get(r, x);
+#pragma unroll
+        for (int i = 0; !whole && i < E; ++i) x[i] = mine(i) ? x[i] : 0.f;
     }
     __device__ __forceinline__ void store(char *base, int64_t at, const float (&x)[E]) const {
         T *row = reinterpret_cast<T *>(base) + at;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            if (FULL || (own[k] == 0 && C >= n)) {
+            if (whole || (vectors && own[k] == 0)) {
                 typename NVec<T>::Raw r;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -97,10 +104,14 @@ template <class T, int TPR, int NV, bool FULL> struct Channels {
                     }
                 }
                 *reinterpret_cast<typename NVec<T>::Raw *>(row + first[k]) = r;
-            } else {
+            }
+            if constexpr (!whole) {
+                const bool part = !vectors || (own[k] > 0 && own[k] < n);
+                if (__builtin_amdgcn_ballot_w64(part)) {     // (in one wave of a row at most)
 #pragma unroll
-                for (int e = 0; e < n; ++e)
-                    if (mine(k * n + e)) row[first[k] + e] = (T)x[k * n + e];
+                    for (int e = 0; e < n; ++e)
+                        if (part && mine(k * n + e)) row[first[k] + e] = (T)x[k * n + e];
+                }
             }
         }
     }
@@ -115,7 +126,7 @@ template <class Ch> __device__ __forceinline__ void channels_of(const Ch &ch, co
     if (!m) {
 #pragma unroll
         for (int i = 0; i < Ch::E; ++i) x[i] = none;
-    } else if (ch.C < n) {
+    } else if constexpr (!Ch::vectors) {
 #pragma unroll
         for (int i = 0; i < Ch::E; ++i) x[i] = ch.mine(i) ? n_mod(m, f32, at + ch.channel(i), none) : none;
     } else if (f32) {
@@ -151,14 +162,14 @@ template <class Ch> __device__ __forceinline__ void channel_factors(const NormAr
 
 // threads of a workgroup: four waves with rows of their own, or one row
 constexpr int norm_threads(int tpr) { return tpr <= 64 ? 256 : tpr; }
+// which of the workgroup's rows a thread works on (the same for a wave, and known to be, where a row has whole waves)
+template <int TPR> __device__ __forceinline__ int norm_row() { return TPR >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : threadIdx.x / TPR; }
 
 // Sums over the TPR threads of a row, K at once, the result in each of them.  lds: K floats a wave of the workgroup, not read or written by another call
 // until a barrier.  The whole workgroup calls.
 template <int TPR, int K> __device__ __forceinline__ void row_sums(float (&v)[K], float *lds) {
 #pragma unroll
-    for (int o = (TPR < 64 ? TPR : 64) / 2; o > 0; o >>= 1)
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], o, 64);
+    for (int k = 0; k < K; ++k) v[k] = lanes_sum<(TPR < 64 ? 16 : 64)>(v[k]);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64, ALL = norm_threads(TPR) / 64;
         const int w = threadIdx.x >> 6, w0 = w / W * W;
@@ -196,9 +207,9 @@ __device__ __forceinline__ void row_stats(const float (&x)[E], const Ch &ch, flo
     r = 1.f / sqrtf(fmaf(s[0], inv_c, eps));
 }
 
-template <class T, int TPR, int NV, bool LAYER, bool FULL>
+template <class T, int TPR, int NV, bool LAYER, int ROW>
 __global__ void __launch_bounds__(norm_threads(TPR)) norm_fwd_kernel(NormArgs a) {
-    using Ch = Channels<T, TPR, NV, FULL>;
+    using Ch = Channels<T, TPR, NV, ROW>;
     constexpr int E = Ch::E, GP = norm_threads(TPR) / TPR;
     __shared__ float lds[4][32];
     const int t = threadIdx.x % TPR, b = blockIdx.y;
@@ -206,7 +217,7 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_fwd_kernel(NormArgs a)
     float gz[E], ga[E], sh[E];
     channel_factors(a, ch, b * a.mod_stride, gz, ga);
     channels_of(ch, a.shift, a.mod_f32, b * a.mod_stride, 0.f, sh);
-    for (int64_t n = (int64_t)blockIdx.x * GP + threadIdx.x / TPR; n < a.N; n += (int64_t)gridDim.x * GP) {
+    for (int64_t n = (int64_t)blockIdx.x * GP + norm_row<TPR>(); n < a.N; n += (int64_t)gridDim.x * GP) {
         const int64_t row = b * a.N + n;
         float x[E], st[4] = {0.f, 0.f, 0.f, 0.f};
         ch.load(a.x, row * a.C, x);
@@ -216,7 +227,7 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_fwd_kernel(NormArgs a)
             if (a.gain_branch) {
                 row_stats<TPR, E, LAYER>(u, ch, a.inv_c, a.eps, lds[0], st[2], st[3]);
 #pragma unroll
-                for (int e = 0; e < E; ++e) u[e] = (u[e] - st[2]) * st[3];
+                for (int e = 0; e < E; ++e) u[e] = (LAYER ? u[e] - st[2] : u[e]) * st[3];
             }
 #pragma unroll
             for (int e = 0; e < E; ++e) x[e] = (float)(T)fmaf(gz[e], u[e], x[e]);
@@ -225,7 +236,7 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_fwd_kernel(NormArgs a)
         if (a.y) {
             row_stats<TPR, E, LAYER>(x, ch, a.inv_c, a.eps, lds[2], st[0], st[1]);
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = fmaf((x[e] - st[0]) * st[1], ga[e], sh[e]);
+            for (int e = 0; e < E; ++e) x[e] = fmaf((LAYER ? x[e] - st[0] : x[e]) * st[1], ga[e], sh[e]);
             ch.store(a.y, row * a.C, x);
         }
         if (a.stats && t == 0) *reinterpret_cast<float4 *>(a.stats + 4 * row) = make_float4(st[0], st[1], st[2], st[3]);
@@ -233,9 +244,9 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_fwd_kernel(NormArgs a)
     }
 }
 
-template <class T, int TPR, int NV, bool LAYER, bool FULL>
+template <class T, int TPR, int NV, bool LAYER, int ROW>
 __global__ void __launch_bounds__(norm_threads(TPR)) norm_bwd_kernel(NormArgs a) {
-    using Ch = Channels<T, TPR, NV, FULL>;
+    using Ch = Channels<T, TPR, NV, ROW>;
     constexpr int E = Ch::E, GP = norm_threads(TPR) / TPR;
     constexpr int SPAN = TPR * E;                            // channels that the threads of a row cover
     __shared__ float lds[2][32];
@@ -246,46 +257,40 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_bwd_kernel(NormArgs a)
     channel_factors(a, ch, b * a.mod_stride, gz, ga);
 #pragma unroll
     for (int i = 0; i < E; ++i) sE[i] = sT[i] = sF[i] = 0.f;
-    // The next row is on its way while this one is worked on (32768 rows of 1024: 93 -> 83 us), but where a thousand threads leave no registers
-    // for it.
-    constexpr bool AHEAD = TPR < 1024;
+    // The next two rows (one where a row is 16 registers a thread and tensor) are on their way while this one is worked on.  Their loads are the same whatever the call
+    // has: a tensor that it lacks stands for x', a row behind the last one for the last one; between loads that may or may not be there the compiler can only wait
+    // for all of them.  For the same reason they are asked for behind this row's stores.
+    constexpr int SLOTS = E * (int)sizeof(T) <= 32 ? 2 : 1;
     const int64_t step = (int64_t)gridDim.x * GP;
-    int64_t n = (int64_t)blockIdx.x * GP + threadIdx.x / TPR;
-    typename Ch::Raw nx, ny, nb, nd;
-    float4 ns;
-    auto ask = [&](int64_t row) {
-        const int64_t at = row * a.C;
-        ns = *reinterpret_cast<const float4 *>(a.stats + 4 * row);
-        if (a.dy) {
-            ch.ask(a.x, at, nx);
-            ch.ask(a.dy, at, ny);
-        }
-        if (a.dx_out) ch.ask(a.dx_out, at, nd);
-        if (a.branch) ch.ask(a.branch, at, nb);
+    int64_t n0 = (int64_t)blockIdx.x * GP + norm_row<TPR>();
+    const char *const in_g = a.dy ? a.dy : a.x, *const in_d = a.dx_out ? a.dx_out : a.x, *const in_u = a.branch ? a.branch : a.x;
+    struct { typename Ch::Raw x, g, d, u; float4 st; } next[SLOTS];
+    auto ask = [&](int64_t n, auto k) {
+        const int64_t row = b * a.N + min(n, a.N - 1), at = row * a.C;
+        next[k].st = *reinterpret_cast<const float4 *>(a.stats + 4 * row);
+        ch.ask(a.x, at, next[k].x);
+        ch.ask(in_g, at, next[k].g);
+        ch.ask(in_d, at, next[k].d);
+        ch.ask(in_u, at, next[k].u);
     };
-    if (AHEAD && n < a.N) ask(b * a.N + n);
-    for (; n < a.N; n += step) {
-        const int64_t row = b * a.N + n, at = row * a.C;
+    auto work = [&](int64_t n, auto k) {
+        const int64_t at = (b * a.N + n) * a.C;
         float d[E], u[E], x[E], g[E];                        // gradient of x'; normed branch; x', dy
-        if (!AHEAD) ask(row);
-        const float4 st = ns;
-        if (a.dy) {
-            ch.get(nx, x);
-            ch.get(ny, g);
-        }
-        if (a.branch) ch.get(nb, u);
-        if (a.dx_out) {
-            ch.get(nd, d);
-        } else {
+        const float4 st = next[k].st;
+        ch.get(next[k].x, x);
+        ch.get(next[k].g, g);
+        ch.get(next[k].d, d);
+        ch.get(next[k].u, u);
+        if (!a.dx_out) {
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] = 0.f;
         }
-        if (AHEAD && n + step < a.N) ask(row + step);
+        if (SLOTS == 1) ask(n + step, k);
         if (a.dy) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                x[e] = (x[e] - st.x) * st.y;                 // not its own: a value that only meets zeros
+                x[e] = (LAYER ? x[e] - st.x : x[e]) * st.y;  // not its own: a value that only meets zeros
                 sE[e] = fmaf(g[e], x[e], sE[e]);
                 sT[e] += g[e];
                 g[e] *= ga[e];
@@ -302,14 +307,14 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_bwd_kernel(NormArgs a)
             m[0] *= a.inv_c;
             m[1] *= a.inv_c;
 #pragma unroll
-            for (int e = 0; e < E; ++e) d[e] = fmaf(st.y, fmaf(-x[e], m[0], g[e]) - m[1], d[e]);
+            for (int e = 0; e < E; ++e) d[e] = fmaf(st.y, LAYER ? fmaf(-x[e], m[0], g[e]) - m[1] : fmaf(-x[e], m[0], g[e]), d[e]);
         }
         ch.store(a.dx, at, d);
         if (a.branch) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                if (a.gain_branch) u[e] = (u[e] - st.z) * st.w;
+                if (a.gain_branch) u[e] = (LAYER ? u[e] - st.z : u[e]) * st.w;
                 sF[e] = fmaf(d[e], u[e], sF[e]);
                 d[e] *= gz[e];
                 m[0] = fmaf(d[e], u[e], m[0]);
@@ -326,11 +331,25 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_bwd_kernel(NormArgs a)
                 m[0] *= a.inv_c;
                 m[1] *= a.inv_c;
 #pragma unroll
-                for (int e = 0; e < E; ++e) d[e] = (fmaf(-u[e], m[0], d[e]) - m[1]) * st.w;
+                for (int e = 0; e < E; ++e) d[e] = (LAYER ? fmaf(-u[e], m[0], d[e]) - m[1] : fmaf(-u[e], m[0], d[e])) * st.w;
             }
             ch.store(a.dbranch, at, d);
         }
+        if (SLOTS == 2) ask(n + 2 * step, k);
         if constexpr (TPR > 64) __syncthreads();             // the next row's sums go where this one's are read
+    };
+    constexpr std::integral_constant<int, 0> k0;
+    constexpr std::integral_constant<int, SLOTS - 1> k1;
+    ask(n0, k0);
+    if (SLOTS == 2) ask(n0 + step, k1);
+    if constexpr (SLOTS == 1) {
+        for (; n0 < a.N; n0 += step) work(n0, k0);
+    } else {                                                 // (two rows a round: one that may leave in between lets the compiler count on no load of the second slot)
+        for (; n0 + step < a.N; n0 += 2 * step) {
+            work(n0, k0);
+            work(n0 + step, k1);
+        }
+        if (n0 < a.N) work(n0, k0);
     }
     if (!a.part) return;
     // the workgroup's sums: its GP rows at a time add theirs in turn
@@ -420,35 +439,42 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(NormArgs a) {
     if (slice == 0 && in && per_channel) per_channel[c] = all;
 }
 
-// The fewest threads a row that hold it with at most `most` channels each, 4 to 64 or whole waves.
-static NormShape norm_shape(const llsa_norm_desc &d, int most, int64_t target) {
+// The fewest threads a row that hold it with at most 16 (backward 8) channels each, 16 or whole waves, up to 512 of them with up to 16 channels.
+// Workgroups: what is resident at once, rows dealt out evenly (fp32 backward, 3 x 2704 rows of 1001: 58 -> 54 us against two workgroups in a second round).  Each
+// workgroup of the backward pass writes sums that are three rows of fp32, so that as soon as every CU has one they get more rows first, up to 8 (16 x 256 rows of 1024
+// 45 -> 37 us, 1 x 2048 24 -> 18, 1 x 1024 22 -> 14; 1 x 256 rows with 8 each 11.3 -> 13.5).
+static NormShape norm_shape(const llsa_norm_desc &d, bool backward) {
+    const int most = backward ? 8 : 16;
+    const int64_t target = backward ? 512 : 1024;            // times 256 threads
     NormShape r;
-    const int vn = d.dtype == LLSA_F32 ? 4 : 8, vec = (d.C + vn - 1) / vn, nv = most / vn;
+    const int vn = d.dtype == LLSA_F32 ? 4 : 8, vec = (d.C + vn - 1) / vn;
     r.tpr = vec <= 16 ? 16 : 64;
-    while (vec > r.tpr * nv) r.tpr *= 2;
+    while (r.tpr < 512 && vec > r.tpr * (most / vn)) r.tpr *= 2;
     r.nv = (vec + r.tpr - 1) / r.tpr;
     if (r.nv == 3) r.nv = 4;
-    const int64_t rows = norm_threads(r.tpr) / r.tpr, all = (d.N + rows - 1) / rows, share = (target * 256 / norm_threads(r.tpr) + d.batch - 1) / d.batch;
-    r.blocks = (int)(all < share ? all : share);
+    const int64_t rows = norm_threads(r.tpr) / r.tpr, all = (d.N + rows - 1) / rows, share = std::max<int64_t>(1, target * 256 / norm_threads(r.tpr) / d.batch);
+    const int64_t least = backward ? std::min<int64_t>(8, (all * d.batch + 255) / 256) : 1, per = std::max(least, (all + share - 1) / share);
+    r.blocks = (int)((all + per - 1) / per);
     return r;
 }
 void norm_layout(NormPlan &p) {
-    p.fwd = norm_shape(p.desc, 16, 1024);
-    p.bwd = norm_shape(p.desc, 8, 512);
+    p.fwd = norm_shape(p.desc, false);
+    p.bwd = norm_shape(p.desc, true);
     p.ws = (size_t)p.desc.batch * p.bwd.blocks * 3 * p.desc.C * sizeof(float);
 }
 
-// As norm_layout chooses: at most 16 channels a thread, 8 in the backward pass
+// As norm_layout chooses: at most 16 channels a thread, 8 in the backward pass but for 512 threads
 template <bool FWD, class F> static void norm_dispatch(const NormPlan &p, const NormShape &sh, F go) {
     using std::integral_constant;
     auto shape = [&](auto t, auto layer) {
         constexpr int vn = 16 / sizeof(t);
         auto with = [&](auto tpr, auto nv) {
-            if (p.desc.C == sh.tpr * sh.nv * vn) go(t, tpr, nv, layer, std::true_type());
-            else go(t, tpr, nv, layer, std::false_type());
+            if (p.desc.C == sh.tpr * sh.nv * vn) go(t, tpr, nv, layer, integral_constant<int, kWhole>());
+            else if (p.desc.C >= vn) go(t, tpr, nv, layer, integral_constant<int, kTail>());
+            else if constexpr (decltype(tpr)::value == 16) go(t, tpr, nv, layer, integral_constant<int, kShort>());
         };
         auto wide = [&](auto tpr) {
-            constexpr int most = (FWD ? 16 : 8) / vn;
+            constexpr int most = (FWD || decltype(tpr)::value == 512 ? 16 : 8) / vn;
             if (sh.nv == 1) with(tpr, integral_constant<int, 1>());
             else if constexpr (most >= 2) {
                 if (sh.nv == 2) with(tpr, integral_constant<int, 2>());
@@ -460,9 +486,7 @@ template <bool FWD, class F> static void norm_dispatch(const NormPlan &p, const 
             case 64: wide(integral_constant<int, 64>()); break;
             case 128: wide(integral_constant<int, 128>()); break;
             case 256: wide(integral_constant<int, 256>()); break;
-            case 512: wide(integral_constant<int, 512>()); break;
-            default:
-                if constexpr (!FWD) wide(integral_constant<int, 1024>());
+            default: wide(integral_constant<int, 512>());
         }
     };
     auto kind = [&](auto t) {
@@ -475,9 +499,9 @@ template <bool FWD, class F> static void norm_dispatch(const NormPlan &p, const 
 
 hipError_t launch_norm_forward(const NormPlan &p, NormArgs a, hipStream_t s) {
     const dim3 grid(p.fwd.blocks, p.desc.batch);
-    norm_dispatch<true>(p, p.fwd, [&](auto t, auto tpr, auto nv, auto layer, auto full) {
+    norm_dispatch<true>(p, p.fwd, [&](auto t, auto tpr, auto nv, auto layer, auto row) {
         constexpr int threads = norm_threads(decltype(tpr)::value);
-        norm_fwd_kernel<decltype(t), decltype(tpr)::value, decltype(nv)::value, decltype(layer)::value, decltype(full)::value><<<grid, threads, 0, s>>>(a);
+        norm_fwd_kernel<decltype(t), decltype(tpr)::value, decltype(nv)::value, decltype(layer)::value, decltype(row)::value><<<grid, threads, 0, s>>>(a);
     });
     return hipGetLastError();
 }
@@ -485,9 +509,9 @@ hipError_t launch_norm_forward(const NormPlan &p, NormArgs a, hipStream_t s) {
 hipError_t launch_norm_backward(const NormPlan &p, NormArgs a, hipStream_t s) {
     const dim3 grid(p.bwd.blocks, p.desc.batch);
     a.blocks = p.bwd.blocks;
-    norm_dispatch<false>(p, p.bwd, [&](auto t, auto tpr, auto nv, auto layer, auto full) {
+    norm_dispatch<false>(p, p.bwd, [&](auto t, auto tpr, auto nv, auto layer, auto row) {
         constexpr int threads = norm_threads(decltype(tpr)::value);
-        norm_bwd_kernel<decltype(t), decltype(tpr)::value, decltype(nv)::value, decltype(layer)::value, decltype(full)::value><<<grid, threads, 0, s>>>(a);
+        norm_bwd_kernel<decltype(t), decltype(tpr)::value, decltype(nv)::value, decltype(layer)::value, decltype(row)::value><<<grid, threads, 0, s>>>(a);
     });
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.part) return e;
