@@ -608,10 +608,9 @@ def norm_backward(p: NormPlan, x_out, dy, stats, branch=None, gain_branch=None, 
              ((gain_branch, "gain_branch"), (gain, "gain")), ((gate, "gate"), (scale, "scale"), (shift, "shift")), dev)
     _chk_vec(stats, "stats", torch.float32, p._stats, dev)
     sums = [None] * 5
-    for i, (t, n, shape) in enumerate(((gain_branch, "dgain_branch", p._vec), (gate, "dgate", p._mods), (gain, "dgain", p._vec),
-                                       (scale, "dscale", p._mods), (shift, "dshift", p._mods))):
-        if t is not None:
-            out[n] = torch.empty(shape, dtype=torch.float32, device=x_out.device)
+    for i, (t, n) in enumerate(((gain_branch, "dgain_branch"), (gate, "dgate"), (gain, "dgain"), (scale, "dscale"), (shift, "dshift"))):
+        if t is not None:                                    # (contiguous; torch.empty takes twice as long, 5 of the 26 us of a call)
+            out[n] = torch.empty_like(t, dtype=torch.float32, memory_format=torch.contiguous_format)
             sums[i] = out[n].data_ptr()
     if workspace is None and any(sums):
         workspace = p.alloc_workspace(x_out.device)
