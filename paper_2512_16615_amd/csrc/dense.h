@@ -39,7 +39,7 @@ struct DensePlan {
 
 // A launch over tiles of rows (or keys) x groups x splits
 struct DenseGrid {
-    FastDiv by_tiles, by_splits, by_rest;      // rest: groups x splits
+    FastDiv by_tiles, by_splits, by_rest, by_heads;      // rest: groups x splits; heads: key heads x splits
     uint32_t wgs, groups;
     int32_t splits, chunk;
     int64_t rows;                   // rows (or keys) of a group

@@ -74,6 +74,7 @@ DenseGrid dense_grid(const DensePlan &p, int64_t rows, const DenseShape &shape, 
     g.by_tiles = FastDiv(tiles);
     g.by_splits = FastDiv(g.splits);
     g.by_rest = FastDiv((int64_t)g.groups * g.splits);
+    g.by_heads = FastDiv((int64_t)p.desc.kv_heads * g.splits);
     g.wgs = (uint32_t)(tiles * g.groups * g.splits);
     g.part = part;
     if (g.splits > 1) g.stat = part + (int64_t)g.splits * g.groups * rows * row_floats;

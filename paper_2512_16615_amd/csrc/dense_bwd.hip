@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dq_waves<T,
     __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];      // wave; stage; keys, values
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const int pair = wave & 3, half = wave >> 2;
-    const DenseWork work = dense_work(grid, a.causal, true);
+    const DenseWork work = dense_work<AXIS, true>(a, grid);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
     const int64_t row0 = (int64_t)work.tile * AXIS, wrow0 = NARROW ? row0 : row0 + pair * 32, r = wrow0 + col;
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dkv_waves<T
     __shared__ __attribute__((aligned(1024))) char lds[LDSB > JOINB ? LDSB : JOINB];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
     const int pair = wave & 3, half = wave >> 2;
-    const DenseWork work = dense_work(grid, a.causal, false);
+    const DenseWork work = dense_work<AXIS, false>(a, grid);
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
     const int key0 = work.tile * AXIS, wkey0 = NARROW ? key0 : key0 + pair * 32, j = wkey0 + col;

@@ -126,6 +126,10 @@ CASES = [
     _case("bf16", 12, 32, 16, 140, 260, 64, causal=True, lens=([140, 3, 0, 77, 128, 129, 140, 1, 64, 65, 100, 139], [260, 3, 5, 0, 256, 257, 70, 260, 64, 33, 100, 1])),
     # and their other axis cut
     _case("bf16", 2, 15, 15, 200, 4200, 128), _case("bf16", 2, 15, 15, 4200, 200, 64), _case("bf16", 2, 30, 15, 100, 6400, 64, causal=True), _case("f32", 2, 15, 15, 200, 4100, 128), _case("f32", 2, 15, 15, 4100, 200, 128),
+    # causal sequences of different lengths, their tiles sorted by work (768 workgroups and more, up to 8 sequences)
+    _case("bf16", 8, 12, 12, 1000, 1000, 64, causal=True, lens=([1000, 0, 130, 700, 1, 999, 128, 300], [1000, 50, 0, 800, 1, 999, 130, 256])),
+    _case("bf16", 5, 40, 20, 600, 513, 128, causal=True, lens=([513, 600, 3, 256, 0], [513, 513, 3, 200, 9])), _case("f32", 3, 44, 44, 700, 700, 32, causal=True, lens=([700, 65, 300], None)),
+    _case("bf16", 2, 60, 60, 150, 900, 32, causal=True, lens=(None, [900, 140])), _case("bf16", 9, 40, 40, 270, 270, 16, causal=True, lens=([270, 1, 0, 5, 128, 129, 200, 270, 64],) * 2),
     # few rows and many keys: the row tiles narrow, the key tiles not
     *[_case("bf16", 1, 4, 4, 1, 5000, d) for d in (32, 64, 128)], _case("bf16", 1, 16, 16, 20, 1100, 64, causal=True), _case("bf16", 10, 16, 16, 33, 130, 128), _case("f32", 1, 16, 16, 20, 1100, 16, causal=True),
     _case("bf16", 8, 32, 32, 30, 300, 64, lens=([30, 1, 0, 15, 30, 30, 29, 2], [300, 300, 300, 0, 129, 128, 1, 64])),
