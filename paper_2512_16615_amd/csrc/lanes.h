@@ -27,4 +27,17 @@ template <int N> __device__ __forceinline__ float lanes_sum(float x) {
     return x;
 }
 
+// The sum of the lanes that are N apart (4 or 16), over the whole wave; lanes 0 .. N - 1 have it
+template <int N> __device__ __forceinline__ float rows_sum(float x) {
+    static_assert(N == 4 || N == 16, "");
+    if constexpr (N == 4) {                                  // 16 lanes turned by 4 and 8
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, true));
+        x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, true));
+    }
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 }  // namespace llsa

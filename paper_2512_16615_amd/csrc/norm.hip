@@ -1,4 +1,4 @@
-// The norms between two blocks with gate and residual, forward and backward: one pass over the rows, each held in registers by 16 to 512
+// The norms between two blocks with gate and residual, forward and backward: one pass over the rows, each held in registers by 4 to 512
 // threads (at most 16 channels a thread), so that a row is read once and written once.  What varies by channel only (the gains, and the
 // modulation of the batch entry that a workgroup belongs to) stays in registers over all rows of the workgroup, combined:
 //   y = n(x') ga + sh, x' = x + gz n(branch)       with ga = gain (1 + scale), sh = shift, gz = alpha gate gain_branch.
@@ -169,7 +169,7 @@ template <int TPR> __device__ __forceinline__ int norm_row() { return TPR >= 64 
 // until a barrier.  The whole workgroup calls.
 template <int TPR, int K> __device__ __forceinline__ void row_sums(float (&v)[K], float *lds) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = lanes_sum<(TPR < 64 ? 16 : 64)>(v[k]);
+    for (int k = 0; k < K; ++k) v[k] = lanes_sum<(TPR < 64 ? TPR : 64)>(v[k]);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64, ALL = norm_threads(TPR) / 64;
         const int w = threadIdx.x >> 6, w0 = w / W * W;
@@ -352,11 +352,20 @@ __global__ void __launch_bounds__(norm_threads(TPR)) norm_bwd_kernel(NormArgs a)
         if (n0 < a.N) work(n0, k0);
     }
     if (!a.part) return;
-    // the workgroup's sums: its GP rows at a time add theirs in turn
+    // the workgroup's sums: a wave's rows add theirs, then the waves in turn
+    if constexpr (TPR < 64) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            sE[e] = rows_sum<TPR>(sE[e]);
+            sT[e] = rows_sum<TPR>(sT[e]);
+            sF[e] = rows_sum<TPR>(sF[e]);
+        }
+    }
     if constexpr (GP > 1) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll 1
-        for (int w = 0; w < GP; ++w) {
-            if ((int)threadIdx.x / TPR == w)
+        for (int w = 0; w < 4; ++w) {
+            if (wave == w && lane < TPR)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     float *s = sums + e * TPR + t;
@@ -439,7 +448,7 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(NormArgs a) {
     if (slice == 0 && in && per_channel) per_channel[c] = all;
 }
 
-// The fewest threads a row that hold it with at most 16 (backward 8) channels each, 16 or whole waves, up to 512 of them with up to 16 channels.
+// The fewest threads a row that hold it with at most 16 (backward 8) channels each, 4, 16 or whole waves, up to 512 of them with up to 16 channels.
 // Workgroups: what is resident at once, rows dealt out evenly (fp32 backward, 3 x 2704 rows of 1001: 58 -> 54 us against two workgroups in a second round).  Each
 // workgroup of the backward pass writes sums that are three rows of fp32, so that as soon as every CU has one they get more rows first, up to 8 (16 x 256 rows of 1024
 // 45 -> 37 us, 1 x 2048 24 -> 18, 1 x 1024 22 -> 14; 1 x 256 rows with 8 each 11.3 -> 13.5).
@@ -448,7 +457,7 @@ static NormShape norm_shape(const llsa_norm_desc &d, bool backward) {
     const int64_t target = backward ? 512 : 1024;            // times 256 threads
     NormShape r;
     const int vn = d.dtype == LLSA_F32 ? 4 : 8, vec = (d.C + vn - 1) / vn;
-    r.tpr = vec <= 16 ? 16 : 64;
+    r.tpr = vec <= 4 ? 4 : vec <= 16 ? 16 : 64;
     while (r.tpr < 512 && vec > r.tpr * (most / vn)) r.tpr *= 2;
     r.nv = (vec + r.tpr - 1) / r.tpr;
     if (r.nv == 3) r.nv = 4;
@@ -471,7 +480,7 @@ template <bool FWD, class F> static void norm_dispatch(const NormPlan &p, const 
         auto with = [&](auto tpr, auto nv) {
             if (p.desc.C == sh.tpr * sh.nv * vn) go(t, tpr, nv, layer, integral_constant<int, kWhole>());
             else if (p.desc.C >= vn) go(t, tpr, nv, layer, integral_constant<int, kTail>());
-            else if constexpr (decltype(tpr)::value == 16) go(t, tpr, nv, layer, integral_constant<int, kShort>());
+            else if constexpr (decltype(tpr)::value == 4) go(t, tpr, nv, layer, integral_constant<int, kShort>());
         };
         auto wide = [&](auto tpr) {
             constexpr int most = (FWD || decltype(tpr)::value == 512 ? 16 : 8) / vn;
@@ -482,6 +491,7 @@ template <bool FWD, class F> static void norm_dispatch(const NormPlan &p, const 
             }
         };
         switch (sh.tpr) {
+            case 4: with(integral_constant<int, 4>(), integral_constant<int, 1>()); break;
             case 16: with(integral_constant<int, 16>(), integral_constant<int, 1>()); break;
             case 64: wide(integral_constant<int, 64>()); break;
             case 128: wide(integral_constant<int, 128>()); break;
