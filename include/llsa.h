@@ -264,14 +264,17 @@ llsa_status llsa_calibrate_copy(const void *src, void *dst, int64_t bytes, void 
  * that no query sees, and every row j >= nk, has a zero gradient.  Such rows are written all the same, and whatever a row behind a
  * length or a key that a query does not see holds, infinities and NaN included, reaches no result.
  *
- * Arithmetic: scores, softmax, sums and gradients in fp32; with bf16 tensors P and dS are rounded to bf16 as operands of their second products (half a
- * step, 2^-8, each), results once.  D = rowsum(dO * O), which the gradients of the scores are relative to, is formed from the stored O; with bf16 the sum of a
- * row's dS then corrects it, for dK everywhere and for dQ where a tile of rows sees 512 keys at most.  Beyond those, dQ of a row that a few keys dominate carries
- * O's rounding (scores of deviation 4, 1024 keys: error 3.5e-3 of dQ in the 2-norm, 2.4e-3 of dK).
+ * Arithmetic: scores, softmax, sums and gradients in fp32; with bf16 tensors P and dS are rounded to bf16 as operands of their
+ * second products (half a step, 2^-8, each), results once.  D = rowsum(dO * O), which the gradients of the scores are relative
+ * to, is formed from the stored O; with bf16 the sum of a row's dS then corrects it, for dK everywhere and for dQ where a tile
+ * of rows sees 512 keys at most.  Beyond those, dQ of a row that a few keys dominate carries O's rounding (scores of deviation
+ * 4, 1024 keys: error 3.5e-3 of dQ in the 2-norm, 2.4e-3 of dK).
  *
- * LLSA_ERR_UNSUPPORTED: other d or types; batch * kv_heads > 65535; Nq, Nkv or Nq * heads / kv_heads > 2^30; more than 2^29 tiles of 32 rows and of 32 keys in all; kernel_path
- * 0 where 256 token strides of K or V, or those and the head strides of a key head's query heads of Q or O, reach 2^32 - 2^20 bytes (offsets inside a tile have 32 bits;
- * between tiles 64).  LLSA_ERR_BAD_SHAPE: sizes below 1, kv_heads that does not divide heads, strides or pointers off the 16-byte grid, a workspace off 256 bytes.
+ * LLSA_ERR_UNSUPPORTED: other d or types; batch * kv_heads > 65535; Nq, Nkv or Nq * heads / kv_heads > 2^30; 2^24 tiles of 128
+ * rows and of 128 keys in all (kernel_path 1: 2^26 rows of a key head, or keys); kernel_path 0 where 256 token strides of K or
+ * V, or those and the head strides of a key head's query heads of Q or O, reach 2^32 - 2^20 bytes (offsets inside a tile have
+ * 32 bits; between tiles 64).  LLSA_ERR_BAD_SHAPE: sizes below 1, kv_heads that does not divide heads, strides or pointers off
+ * the 16-byte grid, a workspace off 256 bytes.
  */
 typedef struct {
     int32_t batch, heads;
@@ -340,8 +343,9 @@ typedef struct {
 } llsa_norm_desc;
 
 typedef struct llsa_norm_plan_s llsa_norm_plan_t;
-/* Host only; as with llsa_dense_plan, host threads and streams may share a plan, and calls that may overlap need a workspace each.  Tensors of [batch, N, C] begin on a 16-byte
-   boundary (the rows need not: C is any number), gains and modulation vectors at any element. */
+/* Host only; as with llsa_dense_plan, host threads and streams may share a plan, and calls that may overlap need a workspace each.
+   Tensors of [batch, N, C] begin on a 16-byte boundary (the rows need not: C is any number), gains and modulation vectors at any
+   element. */
 llsa_status llsa_norm_plan(const llsa_norm_desc *desc, llsa_norm_plan_t **out);
 void llsa_norm_plan_destroy(llsa_norm_plan_t *plan);
 size_t llsa_norm_workspace_bytes(const llsa_norm_plan_t *plan);   /* of llsa_norm_backward; the forward needs none */

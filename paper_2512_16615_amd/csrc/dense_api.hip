@@ -97,7 +97,9 @@ static llsa_status build_dense_plan(const llsa_dense_desc &d, DensePlan &p) {
     // rows and keys are counted in 31 bits, groups are the grid's second dimension
     if (d.Nq > ((int64_t)1 << 30) || d.Nkv > ((int64_t)1 << 30) || d.Nq * p.G > ((int64_t)1 << 30)) return LLSA_ERR_UNSUPPORTED;
     if ((int64_t)d.batch * d.kv_heads > 65535) return LLSA_ERR_UNSUPPORTED;
-    if ((int64_t)d.batch * d.kv_heads * ((d.Nq * p.G + 31) / 32 + (d.Nkv + 31) / 32) >= ((int64_t)1 << 29)) return LLSA_ERR_UNSUPPORTED;   // launch grids
+    // a launch has fewer than 2^32 threads a dimension: 256 for 128 rows or keys of all groups, or 64 for one of a group
+    if (d.kernel_path == 0 && (int64_t)d.batch * d.kv_heads * ((d.Nq * p.G + 127) / 128 + (d.Nkv + 127) / 128) >= ((int64_t)1 << 24)) return LLSA_ERR_UNSUPPORTED;
+    if (d.kernel_path == 1 && std::max<int64_t>(d.Nq * p.G, d.Nkv) >= ((int64_t)1 << 26)) return LLSA_ERR_UNSUPPORTED;
     p.rows = d.Nq * p.G;
     p.elt = d.dtype == LLSA_F32 ? 4 : 2;
     p.scale = d.sm_scale > 0.f ? d.sm_scale : (float)(1.0 / sqrt((double)d.d));

@@ -225,21 +225,20 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dkv_waves<T
     const DenseGroup p(a, work.group);
     const Tile tile(lane);
     const int key0 = work.tile * AXIS, wkey0 = NARROW ? key0 : key0 + pair * 32, j = wkey0 + col;
+    // (of all keys, also those behind the length: on their way before the lengths are there, and what such a key holds stays in its lane)
+    Piece<T> k[Tile::KS], v[Tile::KS];
+    const char *const kj = p.K + min((int64_t)j, a.Nkv - 1) * a.k.token, *const vj = p.V + min((int64_t)j, a.Nkv - 1) * a.v.token;
+#pragma unroll
+    for (int ks = 0; ks < Tile::KS; ++ks) {
+        k[ks].w = *reinterpret_cast<const u32x4 *>(kj + 16 * h + 32 * ks);
+        v[ks].w = *reinterpret_cast<const u32x4 *>(vj + 16 * h + 32 * ks);
+    }
     int first;
     const int steps = dense_row_steps<QT>(a, p, key0, &first);
     const DensePieces piece(grid, work.split, first, steps);
     if (piece.none) return;
     const bool valid = j < p.nk;
-
-    Piece<T> k[KR], v[Tile::KS];
     u32x4 *const spare = reinterpret_cast<u32x4 *>(lds + WAVES * ST * STAGEB + pair * (1024 * SPARE)) + lane;
-#pragma unroll
-    for (int ks = 0; ks < Tile::KS; ++ks) {
-        const u32x4 zero = {0, 0, 0, 0}, x = valid ? *reinterpret_cast<const u32x4 *>(p.K + j * a.k.token + 16 * h + 32 * ks) : zero;
-        if (ks < KR) k[ks].w = x;
-        else spare[64 * (ks - KR)] = x;
-        v[ks].w = valid ? *reinterpret_cast<const u32x4 *>(p.V + j * a.v.token + 16 * h + 32 * ks) : zero;
-    }
     f32x16 dk[Tile::NB], dv[Tile::NB];
 #pragma unroll
     for (int n = 0; n < Tile::NB; ++n)
@@ -263,6 +262,8 @@ __global__ void __launch_bounds__(FORM == kDensePaired ? 512 : 256, (dkv_waves<T
     };
     if (ST == 2 && t0 < piece.t1) fetch(t0);
     loads_done();
+#pragma unroll
+    for (int ks = 0; ks < SPARE; ++ks) spare[64 * ks] = k[KR + ks].w;
     for (int t = t0; t < piece.t1; t += WAVES) {
         if (ST == 1) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

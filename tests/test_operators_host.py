@@ -34,6 +34,7 @@ def test_layouts_match_the_header(llsa):  # noqa: F811
     (dict(o_stride=(0, 64, 512)), 2),           # batch entries of O on top of each other
     (dict(o_stride=(1 << 20, 64, 256)), 2),     # heads 4 .. 7 of a token are heads 0 .. 3 of the next
     (dict(batch=1, heads=60000, Nq=1 << 20), 3),                             # more tiles than a launch takes
+    (dict(batch=2, heads=8, Nq=1 << 27), 3), (dict(batch=1, heads=1, Nkv=1 << 26, kernel_path=1), 3),
     (dict(batch=1, heads=64, kv_heads=1, Nq=1 << 25), 3),
     (dict(k_stride=(1 << 33, 1 << 32, 1 << 23)), 3),                         # 256 tokens 4 GiB apart
     (dict(q_stride=(1 << 34, 1 << 31, 64), kv_heads=4), 3),                  # two heads of a key head 4 GiB apart
