@@ -56,11 +56,13 @@ DenseShape dense_shape(const DensePlan &p, int64_t axis, int64_t other) {
     return r;
 }
 
-// Eight waves a tile, two for each 32 rows, where a CU has one tile anyway (8 x 4096 tokens, d = 128: forward 89 -> 70 us, backward 252 -> 219), or the longest of
-// causal tiles decides (16 x 4096, d = 64, 512 tiles: 60 -> 54 and 169 -> 151; 4 x 16384 212 -> 191 and 627 -> 513).  Beyond that two workgroups of four a CU do better: they
-// wait for each other less (756 tiles, d = 128: 58 us, paired 66).
+// Eight waves a tile, two for each 32 rows, where a CU has one tile anyway (8 x 4096 tokens, d = 128: forward 89 -> 70 us, backward 252 -> 219; 2 x 16 x 1024, d = 64, 51 -> 48 backward) and walks over
+// eight steps at least (8 x 16 heads of 256, four steps: 25 -> 27), or the longest of causal tiles, of 32 steps, decides (16 x 4096, d = 64, 512 tiles: 60 -> 54 and 169 -> 151; 4 x 16384
+// 212 -> 191 and 627 -> 513; 512 tiles of 16 steps 64 -> 70, of 4 32 -> 46 backward).  Beyond that two workgroups of four a CU do better: they wait for each other less (756 tiles, d = 128: 58 us,
+// paired 66).
 bool dense_paired(const DensePlan &p, const DenseShape &shape, int64_t axis) {
-    return (int64_t)p.desc.batch * p.desc.kv_heads * ((axis + 127) / 128) * shape.splits <= (p.desc.causal ? 512 : 256);
+    const int64_t tiles = (int64_t)p.desc.batch * p.desc.kv_heads * ((axis + 127) / 128) * shape.splits;
+    return shape.chunk >= 8 && tiles <= (p.desc.causal && shape.chunk >= 32 ? 512 : 256);
 }
 
 DenseGrid dense_grid(const DensePlan &p, int64_t rows, const DenseShape &shape, int row_floats, float *part) {

@@ -119,7 +119,9 @@ CASES = [
     _case("bf16", 1, 4, 4, 1024, 1024, 64), _case("bf16", 1, 4, 2, 1000, 1100, 128, causal=True), _case("f32", 1, 2, 2, 512, 512, 64), _case("bf16", 1, 2, 2, 700, 700, 32), _case("bf16", 1, 2, 2, 600, 600, 16, causal=True),
     # a sharp softmax: scores of tens
     _case("bf16", 1, 2, 2, 150, 150, 64, sm_scale=1.0), _case("f32", 1, 2, 2, 100, 100, 64, sm_scale=1.0),
-    # many tiles: eight waves a tile (128 to 256 tiles of 128 rows, causal to 512), four waves a tile beyond that
+    # many tiles: eight waves a tile (128 to 256 tiles of 128 rows and eight steps, causal to 512 from 32 steps), four waves a tile otherwise
+    *[_case("bf16", 4, 16, 16, 390, 500, d, causal=c) for d in (16, 32, 64, 128) for c in (False, True)], *[_case("f32", 4, 16, 16, 390, 500, d, causal=True) for d in (16, 32, 64)],
+    *[_case("bf16", 4, 28, 14, 257, 500, d, causal=True, lens=([257, 100, 3, 0], [500, 100, 500, 20]), layout="tokens") for d in (64, 128)], _case("bf16", 2, 10, 10, 2050, 2080, 64, causal=True),
     *[_case("bf16", 4, 16, 16, 200, 200, d, causal=c) for d in (16, 32, 64, 128) for c in (False, True)], *[_case("f32", 4, 16, 16, 200, 200, d, causal=True) for d in (16, 32, 64, 128)],
     *[_case("bf16", 10, 13, 13, 270, 300, d) for d in (16, 32, 64, 128)], *[_case("bf16", 12, 16, 16, 290, 270, d, causal=True) for d in (32, 64, 128)],
     *[_case("f32", 10, 13, 13, 140, 300, d) for d in (16, 32, 64, 128)], _case("bf16", 6, 48, 12, 150, 129, 128, causal=True, layout="tokens"), _case("bf16", 6, 48, 12, 150, 129, 64, layout="piece"),
@@ -145,7 +147,7 @@ def test_dense_against_64_bits(c):
 
 
 MASKED = [("bf16", 64, math.nan, 2, 2, 100, 0), ("bf16", 128, math.inf, 2, 2, 100, 0), ("f32", 32, -math.inf, 2, 2, 100, 0), ("bf16", 16, math.nan, 2, 2, 100, 0),
-          ("bf16", 64, math.nan, 2, 2, 100, 1), ("f32", 128, math.inf, 2, 2, 100, 1), ("bf16", 128, math.nan, 2, 16, 520, 0), ("bf16", 64, math.inf, 2, 64, 520, 0), ("f32", 128, math.nan, 2, 16, 520, 0),
+          ("bf16", 64, math.nan, 2, 2, 100, 1), ("f32", 128, math.inf, 2, 2, 100, 1), ("bf16", 128, math.nan, 2, 16, 520, 0), ("bf16", 64, math.inf, 2, 64, 520, 0), ("bf16", 64, math.nan, 2, 14, 500, 0), ("bf16", 128, math.inf, 2, 14, 500, 0), ("f32", 128, math.nan, 2, 16, 520, 0),
           ("bf16", 64, math.nan, 2, 1, 1800, 0), ("bf16", 128, math.inf, 2, 1, 1800, 0)]
 
 
